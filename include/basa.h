@@ -285,6 +285,73 @@ basa_status basa_varlen_attn(const basa_tensor* q, const basa_tensor* k, const b
                              const int32_t* cu_seqlens, int32_t n_seq, const basa_params* p, void* out,
                              const int64_t* out_strides, void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---- Paged key-value cache, and the attention of single tokens over it ----
+ *
+ * A cache holds K and V in `pages` pages of `page` tokens: two basa_tensor descriptors with batch = pages, L = page (any page
+ * size from 1 on) and free strides, so that a page may be stored head by head ([pages, heads, page, d]) or token by token
+ * ([pages, page, heads, d]).  Sequence i owns the pages named in row i of a block table, int32 [n_seq, width] with rows
+ * table_stride >= width entries apart: its token t lives in page table[i][t / page] at place t % page, which is slot
+ * table[i][t / page] * page + t % page.  Sequences may share pages that are only read.  Tables, slots, lengths and offsets are
+ * device data that the host cannot check: a page id outside [0, pages) and a slot outside [0, pages * page) are no page
+ * and no slot (what that means stands at each call), never an access outside the caller's tensors.  One table row holds at most
+ * 2^30 tokens.
+ */
+
+/*
+ * Block tables and slot maps of one step.  Sequence i holds have[i] tokens and gets add[i] more (negative numbers count as 0); its
+ * new tokens are rows cu_add[i] .. cu_add[i] + add[i] - 1 of the step's packed batch, in order of i.  A sequence is served
+ * if its tokens fit its table row, its rows fit the slot map, and the free pages that it and the sequences before it need are
+ * there.  A served sequence needs ceil((have + add) / page) - ceil(have / page) pages; it gets them in order of i from the start of free_pages,
+ * they are entered in its table row behind the pages that it holds, and every new token gets its slot.  One that is not
+ * served keeps its length and its table row, and its new tokens have no slot.
+ *   have, add    [n_seq] int32, n_seq <= 8192.
+ *   table        in and out, [n_seq, width]: entries of pages that are opened are written, the others left as they were.
+ *   free_pages   [n_free] int32: pages that belong to no one, each once.
+ *   slots        out [n_slots] int64: the slot of every row, -1 for a row without one: of a sequence that is not served, behind an
+ *                entry of the table that is negative, or behind the last sequence.
+ *   lens         out [n_seq] int32: have + add, or have of a sequence that is not served.
+ *   cu_add       out [n_seq + 1] int32: running sum of add (cut at 2^31 - 1).
+ *   pages        out [2] int32: how many of free_pages were given out (the first ones), and how many would have been if none were short.
+ * No output may overlap an input or another output: a step that goes on from its own result keeps two sets, or copies.
+ */
+basa_status basa_page_tables(const int32_t* have, const int32_t* add, int32_t n_seq, int32_t page, int32_t* table, int32_t width,
+                             int64_t table_stride, const int32_t* free_pages, int32_t n_free, int64_t* slots, int32_t n_slots,
+                             int32_t* lens, int32_t* cu_add, int32_t* pages, void* stream);
+/*
+ * Packed rows k and v ([1, heads, T, d] descriptors, free strides) into the pages: row t goes to slots[t] (int64 [T]); a row
+ * whose slot is none is left out.  No slot may be named twice in a call (whose bytes it holds then is not defined), and k and v must
+ * not overlap the pages.
+ */
+basa_status basa_cache_append(const basa_tensor* k, const basa_tensor* v, const int64_t* slots, const basa_tensor* k_pages,
+                              const basa_tensor* v_pages, void* stream);
+/*
+ * Cached rows out of the pages: rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 of k and v ([1, heads, T, d] descriptors, written) are tokens
+ * 0, 1, ... of sequence i.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending.  A row whose page is none is zero; rows before
+ * cu_seqlens[0] and from cu_seqlens[n_seq] on are left as they were.  k and v must not overlap each other or the pages.
+ */
+basa_status basa_cache_gather(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                              int64_t table_stride, const int32_t* cu_seqlens, int32_t n_seq, const basa_tensor* k, const basa_tensor* v,
+                              void* stream);
+/*
+ * Attention (Eq. 1) of one new token of every sequence over the first lens[i] tokens of its pages (the new one among them, once it was
+ * appended), all of them: what the block-sparse prefill of a prompt is followed by.
+ *   q            [batch, heads_q, 1, d]; sequence i is batch entry i.  Query head h reads KV head h / (heads_q / heads_kv).
+ *   lens         [batch] int32; lengths below 0 count as 0, lengths beyond width * page as that.
+ *   out          [batch, heads_q, d], dtype of q, 16-byte aligned.  out_strides: nullable HOST array of 2, strides of its batch and
+ *                head axes in elements (multiples of 16 bytes, head stride >= d).  Rows of out must not alias each other or an input.
+ *   lse          out, nullable, [batch, heads_q] float.
+ *   ws           workspace of basa_decode_workspace_size() bytes.  Nothing in it has to start at zero.
+ * Tokens of a page that is none carry no weight, whatever the rows behind them hold; a query without any token gets a zero row and lse
+ * = -inf, as does one whose scores are all -inf.  Accumulation, softmax state and partial results in fp32; with bf16 tensors the weights
+ * enter the second product as the sum of two bf16 numbers.  Long sequences are split over workgroups: where goes by the lengths of the
+ * whole call, so that a sequence agrees with itself called alone within rounding; repeating a call gives the same bits.
+ */
+size_t basa_decode_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t width);
+basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table,
+                             int32_t width, int64_t table_stride, const int32_t* lens, void* out, const int64_t* out_strides, float* lse,
+                             void* ws, size_t ws_bytes, void* stream);
+
 /* Reason of the last non-OK status returned on this thread (host string, owned by the
  * library, valid until the next failing call on the thread). */
 const char* basa_last_error(void);

@@ -7,6 +7,7 @@ loaded the first call raises: there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -29,6 +30,7 @@ EXPORTS = (
     "basa_profile_read", "basa_calibrate_mfma", "basa_calibrate_read", "basa_block_mass_workspace_size", "basa_block_mass",
     "basa_block_radius", "basa_deviation_bound", "basa_selection_fidelity", "basa_pearson_sums",
     "basa_attn_best_workspace_size", "basa_varlen_workspace_size", "basa_varlen_attn", "basa_static_scratch_size", "basa_static_init", "basa_norm_sort_static",
+    "basa_page_tables", "basa_cache_append", "basa_cache_gather", "basa_decode_workspace_size", "basa_decode_attn",
 )
 
 
@@ -123,6 +125,16 @@ def load():
     lib.basa_selection_fidelity.argtypes = [V, V, V, C.c_int64, C.c_int32, V, V, V]
     lib.basa_pearson_sums.restype = C.c_int
     lib.basa_pearson_sums.argtypes = [V, V, C.c_int64, V, V]
+    lib.basa_page_tables.restype = C.c_int
+    lib.basa_page_tables.argtypes = [V, V, C.c_int32, C.c_int32, V, C.c_int32, C.c_int64, V, C.c_int32, V, C.c_int32, V, V, V, V]
+    lib.basa_cache_append.restype = C.c_int
+    lib.basa_cache_append.argtypes = [T, T, V, T, T, V]
+    lib.basa_cache_gather.restype = C.c_int
+    lib.basa_cache_gather.argtypes = [T, T, V, C.c_int32, C.c_int64, V, C.c_int32, T, T, V]
+    lib.basa_decode_workspace_size.restype = C.c_size_t
+    lib.basa_decode_workspace_size.argtypes = [T, T, T, C.c_int32]
+    lib.basa_decode_attn.restype = C.c_int
+    lib.basa_decode_attn.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, S3, V, V, C.c_size_t, V]
     lib.basa_calibrate_read.restype = C.c_int
     lib.basa_calibrate_read.argtypes = [V, C.c_size_t, V, V]
     lib.basa_calibrate_mfma.restype = C.c_int
@@ -404,6 +416,182 @@ def ba_att_varlen(q, k, v, cu_seqlens, block: int = 128, sparsity: float = 0.5, 
 def _varlen_params(block, sparsity, beta: float = 1.0, sort: int = SORT_QK, window: int = 0, mass_target: float = 0.0,
                    min_keep: int = 0, segments=None, causal: bool = False):
     return params(block, sparsity, beta, sort, window, mass_target, min_keep, causal=causal)
+
+
+# ---------------------------------------------------------------- paged key-value cache
+class PagedCache:
+    """Keys and values in pages, indexed [pages, heads_kv, page, d]: the two tensors and their descriptors.  Any strides with a
+    contiguous d axis (a token-major store [pages, page, heads_kv, d] comes as its permute(0, 2, 1, 3))."""
+    __slots__ = ("k", "v", "device", "dtype", "pages", "heads", "page", "d", "_kd", "_vd", "_keys")
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        self._kd, self._vd = tensor_desc(k), tensor_desc(v)
+        if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
+            raise ValueError("keys and values must agree in shape, dtype and device")
+        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
+        self.pages, self.heads, self.page, self.d = k.shape
+        self._keys = C.byref(self._kd), C.byref(self._vd)
+
+
+class PageTables:
+    """Outputs of basa_page_tables (device tensors) for n_seq sequences and up to `tokens` new tokens."""
+    __slots__ = ("slots", "lens", "cu", "pages")
+
+    def __init__(self, n_seq: int, tokens: int, device):
+        self.slots = torch.empty(tokens, dtype=torch.int64, device=device)
+        self.lens = torch.empty(n_seq, dtype=torch.int32, device=device)
+        self.cu = torch.empty(n_seq + 1, dtype=torch.int32, device=device)
+        self.pages = torch.empty(2, dtype=torch.int32, device=device)
+
+
+def _int_array(t: torch.Tensor, name: str, device, shape, dtype=torch.int32):
+    """An array of device integers as the kernels take it: its pointer."""
+    if t.dtype != dtype or t.device != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on {device}")
+    return t.data_ptr()
+
+
+def _block_table(table: torch.Tensor, n_seq: int, device):
+    """(pointer, width, row stride) of a block table [n_seq, width]."""
+    if table.dim() != 2 or table.dtype != torch.int32 or table.device != device or table.shape[0] != n_seq or \
+            (table.numel() > 1 and table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError(f"the block table must be an int32 tensor [{n_seq}, width] on {device} with contiguous rows")
+    width = table.shape[1]
+    return table.data_ptr(), width, table.stride(0) if n_seq > 1 else max(width, table.stride(0))
+
+
+def _packed_desc(x: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
+    """Descriptor of packed rows [T, heads_kv, d] that belong to a cache."""
+    if x.dim() != 3 or x.shape[1] != cache.heads or x.shape[2] != cache.d or x.dtype != cache.dtype or x.device != cache.device:
+        raise ValueError(f"{name} must be a {cache.dtype} tensor [tokens, {cache.heads}, {cache.d}] on {cache.device}")
+    if x.stride(2) != 1:
+        raise ValueError(f"{name}: the head dimension must be contiguous")
+    T, h, d = x.shape
+    st, sh = x.stride(0) if T > 1 else max(d, x.stride(0)), x.stride(1)
+    return BasaTensor(x.data_ptr(), _DTYPES[x.dtype], 1, h, T, d, 0, sh if h > 1 else 0, st)
+
+
+def _on_device(device):
+    """The device of a call's tensors as the current one, which its stream and its launches belong to."""
+    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def basa_page_tables(have, add, table, free_pages, page: int, tokens: int, out: Optional[PageTables] = None) -> PageTables:
+    """Block tables (`table`, written in place) and slots of a step in which sequence i of have[i] tokens gets add[i] more; `tokens`: rows of
+    the step's packed batch, at least sum(add) for every sequence to be served."""
+    lib, dev, n = load(), table.device, have.shape[0]
+    tab, width, stride = _block_table(table, n, dev)
+    if out is None:
+        out = PageTables(n, int(tokens), dev)
+    one = (n,)
+    args = (_int_array(have, "have", dev, one), _int_array(add, "add", dev, one), n, int(page), tab, width, stride,
+            _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0],
+            _int_array(out.slots, "slots", dev, (int(tokens),), torch.int64), int(tokens), _int_array(out.lens, "lens", dev, one),
+            _int_array(out.cu, "cu", dev, (n + 1,)), _int_array(out.pages, "pages", dev, (2,)))
+    with _on_device(dev):
+        _check(lib.basa_page_tables(*args, _stream(table)))
+    return out
+
+
+def basa_cache_append(k, v, slots, cache: PagedCache):
+    """Packed rows k, v [T, heads_kv, d] into the slots of the cache that `slots` [T] names; a negative slot leaves its row out."""
+    kd, vd = _packed_desc(k, "k", cache), _packed_desc(v, "v", cache)
+    if v.shape != k.shape:
+        raise ValueError("v must have the shape of k")
+    at = _int_array(slots, "slots", cache.device, k.shape[:1], torch.int64)
+    if k.shape[0] == 0:
+        return
+    with _on_device(cache.device):
+        _check(load().basa_cache_append(C.byref(kd), C.byref(vd), at, *cache._keys, _stream(k)))
+
+
+def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=None):
+    """(k, v), packed rows [tokens, heads_kv, d]: rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 (a device tensor) are the first tokens of sequence
+    i.  `out`: the two tensors to write into."""
+    n = cu_seqlens.shape[0] - 1
+    tab, width, stride = _block_table(table, n, cache.device)
+    cu = _int_array(cu_seqlens, "cu_seqlens", cache.device, (n + 1,))
+    if out is None:
+        shape = (int(tokens), cache.heads, cache.d)
+        out = tuple(torch.empty(shape, dtype=cache.dtype, device=cache.device) for _ in range(2))
+    k, v = out
+    kd, vd = _packed_desc(k, "k", cache), _packed_desc(v, "v", cache)
+    if k.shape[0] != tokens or v.shape != k.shape:
+        raise ValueError("out: two tensors of `tokens` rows")
+    if tokens:
+        with _on_device(cache.device):
+            _check(load().basa_cache_gather(*cache._keys, tab, width, stride, cu, n, C.byref(kd), C.byref(vd), _stream(k)))
+    return k, v
+
+
+def _token_desc(q: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
+    """Descriptor of one token per sequence, [batch, heads, d]."""
+    if q.dim() != 3 or q.dtype != cache.dtype or q.device != cache.device or q.stride(2) != 1:
+        raise ValueError(f"{name} must be a {cache.dtype} tensor [batch, heads, d] on {cache.device} with a contiguous d axis")
+    b, h, d = q.shape
+    return BasaTensor(q.data_ptr(), _DTYPES[q.dtype], b, h, 1, d, q.stride(0) if b > 1 else 0, q.stride(1) if h > 1 else 0, d)
+
+
+def decode_workspace_size(q, cache: PagedCache, table) -> int:
+    """Bytes of workspace for basa_decode_attn with tables of this width."""
+    return int(load().basa_decode_workspace_size(C.byref(_token_desc(q, "q", cache)), *cache._keys, table.shape[1]))
+
+
+def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, ws=None, out=None):
+    """Attention of one new token of every sequence, q [batch, heads_q, d], over the first lens[i] tokens of its pages."""
+    lib, dev = load(), cache.device
+    qd = _token_desc(q, "q", cache)
+    b, hq, d = q.shape
+    tab, width, stride = _block_table(table, b, dev)
+    at = _int_array(lens, "lens", dev, (b,))
+    if out is None:
+        out = torch.empty((b, hq, d), dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or out.stride(2) != 1:
+        raise ValueError("out must have the shape, dtype and device of q and a contiguous d axis")
+    lse = torch.empty((b, hq), dtype=torch.float32, device=dev) if want_lse else None
+    if b:
+        qr = C.byref(qd)
+        if ws is None:
+            ws = _ws(lib.basa_decode_workspace_size(qr, *cache._keys, width), dev)
+        ostr = (C.c_int64 * 2)(out.stride(0) if b > 1 else 0, out.stride(1) if hq > 1 else d)
+        with _on_device(dev):
+            _check(lib.basa_decode_attn(qr, *cache._keys, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel(),
+                                        _stream(q)))
+    return (out, lse) if want_lse else out
+
+
+def ba_att_decode(q, k, v, cache: PagedCache, table, lens, slots, want_lse: bool = False, ws=None, out=None):
+    """One layer of a decode step: the new token of every sequence, q [batch, heads_q, d] and k, v [batch, heads_kv, d], enters the cache at
+    its slot and attends to everything that its sequence holds.  table, lens, slots: of basa_page_tables, once for all layers."""
+    basa_cache_append(k, v, slots, cache)
+    return basa_decode_attn(q, cache, table, lens, want_lse, ws, out)
+
+
+def ba_att_cached(q, k, v, cu_seqlens, cache: PagedCache, table, slots, cached=None, block: int = 128, sparsity: float = 0.5, **kw):
+    """ba_att_varlen over a packed batch of prompts whose keys and values enter the cache: sequence i has rows cu_seqlens[i] ..
+    cu_seqlens[i + 1] - 1 (host list) of q, k and v.  cached: host list of the tokens that a sequence held before; its new queries then meet
+    all of them, read back from the pages, and the new ones (`causal` counts from the end: the last query sees every key)."""
+    cu = [int(t) for t in cu_seqlens]
+    before = [0] * (len(cu) - 1) if cached is None else [int(t) for t in cached]
+    if len(before) != len(cu) - 1 or any(t < 0 for t in before):
+        raise ValueError("cached: a length >= 0 for every sequence")
+    if cu[0] < 0 or any(a > b for a, b in zip(cu[:-1], cu[1:])) or cu[-1] > q.shape[0]:
+        raise ValueError(f"cu_seqlens must ascend within [0, {q.shape[0]}]")
+    basa_cache_append(k, v, slots, cache)
+    if not any(before):
+        return ba_att_varlen(q, k, v, cu, block, sparsity, **kw)
+    ends = [0]
+    for i, t in enumerate(before):
+        new = cu[i + 1] - cu[i]
+        ends.append(ends[-1] + (t + new if new else 0))          # a sequence without new rows reads nothing
+    ck, cv = basa_cache_gather(cache, table, torch.tensor(ends, dtype=torch.int32, device=cache.device), ends[-1])
+    out = torch.empty_like(q)
+    view = lambda x, a, b: x[a:b].permute(1, 0, 2).unsqueeze(0)          # [1, heads, L, d], no copy
+    for i, (a, b) in enumerate(zip(cu[:-1], cu[1:])):
+        if b > a:
+            e0, e1 = ends[i], ends[i + 1]
+            ba_att(view(q, a, b), view(ck, e0, e1), view(cv, e0, e1), block, sparsity, out=view(out, a, b), **kw)
+    return out
 
 
 def basa_profile_enable(on: bool):

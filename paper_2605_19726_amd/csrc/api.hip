@@ -35,7 +35,8 @@ std::vector<ProfRec> g_prof_recs;
 const char* const kKernelNames[K_COUNT] = {
     "norm_tile_sort_kernel", "merge_pass_kernel", "block_stats_kernel",
     "block_scores_kernel", "row_select_kernel", "gather_kernels", "attn_mfma_kernel",
-    "attn_f32_kernel", "block_mass_kernel", "diagnostic_small_kernels", "scores_select_kernel", "attn_combine_kernel"};
+    "attn_f32_kernel", "block_mass_kernel", "diagnostic_small_kernels", "scores_select_kernel", "attn_combine_kernel",
+    "paged_cache_kernels", "decode_kernel", "decode_join_kernel"};
 }  // namespace
 
 ProfScope::ProfScope(int id, hipStream_t st) : slot_(-1), st_(st) {
@@ -65,7 +66,8 @@ int kappa_of(int n_k, double s) {
   return k < 1 ? 1 : k;
 }
 
-basa_status check_tensor(const basa_tensor* t, const char* name) {
+// The checks that packed tensors and the pages of a cache share: everything but the size of the grid.
+basa_status check_rows(const basa_tensor* t, const char* name) {
   if (!t) { set_error("%s: null tensor descriptor", name); return BASA_ERR_INVALID_ARG; }
   if (!t->ptr) { set_error("%s: null data pointer", name); return BASA_ERR_INVALID_ARG; }
   if (t->dtype != BASA_F32 && t->dtype != BASA_BF16) {
@@ -87,6 +89,12 @@ basa_status check_tensor(const basa_tensor* t, const char* name) {
   if (reinterpret_cast<uintptr_t>(t->ptr) % 16) {
     set_error("%s: data pointer must be 16-byte aligned", name); return BASA_ERR_INVALID_ARG;
   }
+  return BASA_OK;
+}
+
+basa_status check_tensor(const basa_tensor* t, const char* name) {
+  const basa_status s = check_rows(t, name);
+  if (s != BASA_OK) return s;
   if ((int64_t)t->batch * t->heads > 65535) {
     set_error("%s: batch*heads exceeds 65535", name); return BASA_ERR_UNSUPPORTED;
   }
@@ -340,6 +348,66 @@ basa_status check_varlen(const basa_tensor* q, const basa_tensor* k, const basa_
       return BASA_ERR_INVALID_ARG;
     }
   return BASA_OK;
+}
+
+// ---- paged key-value cache ------------------------------------------------------------------
+// Largest counts that the kernels take as 32-bit numbers with room for a step beyond them.
+constexpr int kMaxPagedTokens = 1 << 30;
+
+basa_status check_pages(const basa_tensor* k, const basa_tensor* v) {
+  basa_status s;
+  if ((s = check_rows(k, "k_pages")) != BASA_OK) return s;
+  if ((s = check_rows(v, "v_pages")) != BASA_OK) return s;
+  if (v->dtype != k->dtype || v->d != k->d || v->batch != k->batch || v->heads != k->heads || v->L != k->L) {
+    set_error("v_pages must have the shape and dtype of k_pages"); return BASA_ERR_INVALID_ARG;
+  }
+  if (k->heads > 65535) { set_error("k_pages: more than 65535 heads"); return BASA_ERR_UNSUPPORTED; }
+  return BASA_OK;
+}
+// A block table of n_seq rows of `width` page ids, for pages of `page` tokens.
+basa_status check_table(const int32_t* table, int32_t n_seq, int32_t width, int64_t table_stride, int32_t page) {
+  if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
+  if (!table && n_seq > 0) { set_error("null block table"); return BASA_ERR_INVALID_ARG; }
+  if (width < 1 || table_stride < width) {
+    set_error("a block table needs width >= 1 and a row stride >= width (got %d, %lld)", width, (long long)table_stride);
+    return BASA_ERR_INVALID_ARG;
+  }
+  if ((int64_t)width * page > kMaxPagedTokens) {
+    set_error("block table rows of %d pages of %d tokens exceed %d tokens", width, page, kMaxPagedTokens); return BASA_ERR_UNSUPPORTED;
+  }
+  return BASA_OK;
+}
+// Packed rows of k and v next to the pages that they come from or go to.
+basa_status check_packed(const basa_tensor* k, const basa_tensor* v, const basa_tensor* k_pages, const basa_tensor* v_pages) {
+  basa_status s;
+  if ((s = check_pages(k_pages, v_pages)) != BASA_OK) return s;
+  if ((s = check_rows(k, "k")) != BASA_OK) return s;
+  if ((s = check_rows(v, "v")) != BASA_OK) return s;
+  if (v->dtype != k->dtype || v->d != k->d || v->batch != k->batch || v->heads != k->heads || v->L != k->L) {
+    set_error("v must have the shape and dtype of k"); return BASA_ERR_INVALID_ARG;
+  }
+  if (k->batch != 1 || k->dtype != k_pages->dtype || k->d != k_pages->d || k->heads != k_pages->heads) {
+    set_error("packed rows have batch 1 and the dtype, heads and head dimension of the pages"); return BASA_ERR_INVALID_ARG;
+  }
+  if (k->L > kMaxPagedTokens) { set_error("more than %d tokens in a call", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
+  return BASA_OK;
+}
+bool overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + b_bytes && y < x + a_bytes;
+}
+basa_status check_decode(const basa_tensor* q, const basa_tensor* k, const basa_tensor* v, int32_t width) {
+  basa_status s;
+  if ((s = check_rows(q, "q")) != BASA_OK) return s;
+  if ((s = check_pages(k, v)) != BASA_OK) return s;
+  if (q->L != 1) { set_error("q: one token of every sequence (L = 1), got L = %d", q->L); return BASA_ERR_INVALID_ARG; }
+  if (q->dtype != k->dtype || q->d != k->d) { set_error("q and the pages must agree in dtype and head dimension"); return BASA_ERR_INVALID_ARG; }
+  if (q->heads % k->heads != 0) {
+    set_error("query heads (%d) must be a multiple of kv heads (%d)", q->heads, k->heads); return BASA_ERR_INVALID_ARG;
+  }
+  if ((int64_t)q->batch * q->heads > kMaxPagedTokens) { set_error("q: batch*heads exceeds %d", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
+  static const int32_t some = 0;
+  return check_table(&some, q->batch, width, width, k->L);
 }
 
 }  // namespace
@@ -669,6 +737,91 @@ basa_status basa_norm_sort_static(const basa_tensor* x, const basa_params* p, in
   s = launch_norm_sort(xv, p->window, segs, perm, keys_out, ptr, rows_cached(xv), reinterpret_cast<hipStream_t>(stream));
   t_prof_off = false;
   return s;
+}
+
+}  // extern "C"
+
+// ---- paged key-value cache ------------------------------------------------------------------
+extern "C" {
+
+basa_status basa_page_tables(const int32_t* have, const int32_t* add, int32_t n_seq, int32_t page, int32_t* table, int32_t width,
+                             int64_t table_stride, const int32_t* free_pages, int32_t n_free, int64_t* slots, int32_t n_slots,
+                             int32_t* lens, int32_t* cu_add, int32_t* pages, void* stream) {
+  basa_status s;
+  if (page < 1) { set_error("page size %d must be >= 1", page); return BASA_ERR_INVALID_ARG; }
+  if ((s = check_table(table, n_seq, width, table_stride, page)) != BASA_OK) return s;
+  if (!page_tables_take(n_seq)) { set_error("more sequences (%d) than a call takes", n_seq); return BASA_ERR_UNSUPPORTED; }
+  if (n_seq > 0 && (!have || !add || !lens)) { set_error("null have, add or lens"); return BASA_ERR_INVALID_ARG; }
+  if (!cu_add || !pages) { set_error("null cu_add or pages"); return BASA_ERR_INVALID_ARG; }
+  if (n_free < 0 || (n_free > 0 && !free_pages)) { set_error("null free_pages, or a negative number of them (%d)", n_free); return BASA_ERR_INVALID_ARG; }
+  if (n_slots < 0 || (n_slots > 0 && !slots)) { set_error("null slots, or a negative number of them (%d)", n_slots); return BASA_ERR_INVALID_ARG; }
+  if (n_slots > kMaxPagedTokens) { set_error("more than %d slots in a call", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
+  // every workgroup reads all lengths: none of them may be written meanwhile
+  struct Span { const void* at; size_t bytes; const char* name; };
+  const size_t table_bytes = n_seq > 0 ? ((size_t)(n_seq - 1) * table_stride + width) * 4 : 0;
+  const Span in[] = {{have, (size_t)n_seq * 4, "have"}, {add, (size_t)n_seq * 4, "add"}, {free_pages, (size_t)n_free * 4, "free_pages"}};
+  const Span out[] = {{lens, (size_t)n_seq * 4, "lens"}, {cu_add, ((size_t)n_seq + 1) * 4, "cu_add"}, {pages, 8, "pages"},
+                      {slots, (size_t)n_slots * 8, "slots"}, {table, table_bytes, "table"}};
+  for (const Span& o : out) {
+    for (const Span& i : in)
+      if (overlap(o.at, o.bytes, i.at, i.bytes)) { set_error("%s must not overlap %s", o.name, i.name); return BASA_ERR_INVALID_ARG; }
+    for (const Span* p = out; p != &o; ++p)
+      if (overlap(o.at, o.bytes, p->at, p->bytes)) { set_error("%s must not overlap %s", o.name, p->name); return BASA_ERR_INVALID_ARG; }
+  }
+  return launch_page_tables(have, add, n_seq, page, table, width, table_stride, free_pages, n_free, slots, n_slots, lens, cu_add, pages,
+                            reinterpret_cast<hipStream_t>(stream));
+}
+
+basa_status basa_cache_append(const basa_tensor* k, const basa_tensor* v, const int64_t* slots, const basa_tensor* k_pages,
+                              const basa_tensor* v_pages, void* stream) {
+  const basa_status s = check_packed(k, v, k_pages, v_pages);
+  if (s != BASA_OK) return s;
+  if (!slots) { set_error("null slots"); return BASA_ERR_INVALID_ARG; }
+  return launch_cache_append(view_of(*k), view_of(*v), slots, view_of(*k_pages), view_of(*v_pages), reinterpret_cast<hipStream_t>(stream));
+}
+
+basa_status basa_cache_gather(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                              int64_t table_stride, const int32_t* cu_seqlens, int32_t n_seq, const basa_tensor* k, const basa_tensor* v,
+                              void* stream) {
+  basa_status s = check_packed(k, v, k_pages, v_pages);
+  if (s != BASA_OK) return s;
+  if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
+  if (!cu_seqlens) { set_error("null cu_seqlens"); return BASA_ERR_INVALID_ARG; }
+  return launch_cache_gather(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, cu_seqlens, n_seq, view_of(*k), view_of(*v),
+                             reinterpret_cast<hipStream_t>(stream));
+}
+
+size_t basa_decode_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t width) {
+  if (check_decode(q, k_pages, v_pages, width) != BASA_OK) return 0;
+  return decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, (int64_t)width * k_pages->L);
+}
+
+basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table,
+                             int32_t width, int64_t table_stride, const int32_t* lens, void* out, const int64_t* out_strides, float* lse,
+                             void* ws, size_t ws_bytes, void* stream) {
+  basa_status s;
+  if ((s = check_decode(q, k_pages, v_pages, width)) != BASA_OK) return s;
+  if ((s = check_table(table, q->batch, width, table_stride, k_pages->L)) != BASA_OK) return s;
+  if (!lens) { set_error("null lens"); return BASA_ERR_INVALID_ARG; }
+  if (!out) { set_error("null output pointer"); return BASA_ERR_INVALID_ARG; }
+  if (reinterpret_cast<uintptr_t>(out) % 16) { set_error("out must be 16-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  int64_t out_b = (int64_t)q->heads * q->d, out_h = q->d;
+  if (out_strides) {
+    const int64_t per16 = q->dtype == BASA_BF16 ? 8 : 4;
+    out_b = out_strides[0]; out_h = out_strides[1];
+    if (out_h < q->d || out_h % per16 || out_b % per16 || out_b < 0) {
+      set_error("out_strides must be non-negative multiples of 16 bytes with the head stride >= d");
+      return BASA_ERR_INVALID_ARG;
+    }
+  }
+  const size_t need = decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, (int64_t)width * k_pages->L);
+  if (!ws || ws_bytes < need) {
+    set_error("decode workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
+    return BASA_ERR_WORKSPACE;
+  }
+  if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  return launch_decode_attn(view_of(*q), view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, out, out_b, out_h, lse, ws,
+                            reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

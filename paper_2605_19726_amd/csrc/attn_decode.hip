@@ -1,0 +1,469 @@
+// Attention of one new token of every sequence over its pages of the key-value cache (gfx950).
+//
+// For a sequence of n cached tokens and a query head h of KV head h / group:  s_j = q . k_j,  m = max_j s_j,
+// o = sum_j e^((s_j - m) / sqrt(d)) v_j / sum_j e^((s_j - m) / sqrt(d)),  lse = m / sqrt(d) + ln sum.  One pass over the cache with a
+// running maximum and sum per query head.  4 group flops for 2 bytes of bf16: bound by the memory up to a group of several hundred, so that
+// everything serves the loads: the matrix instruction takes the query heads of a KV head as its 16 columns, used or not.
+//
+// Operands straight from memory, no LDS in between.  A wave takes 32 tokens at a time.  S^T = K Q^T: lane (g, r) of the A operand
+// holds 16 bytes of token r, chunk 4 c + g of its row at step c; the queries are laid out alike.  Of the result, lane (g, n) holds tokens
+// 4 g .. 4 g + 3 of each half for query head n: as they are, the B operand of O^T += V^T P^T, if token order within the sum is that
+// of lane group g: its own eight tokens.  The A operand is eight tokens of one dimension: lane (g, r) loads its group's eight
+// tokens, chunk r of each row (whole rows, 16 lanes of 16 bytes), and turns its 8 x 8 block in registers, a byte permutation for two
+// numbers; output block e holds dimensions 8 r + e.  The running maximum is that of the lane's own column in every lane.
+// bf16: P goes in as the sum of two bf16 numbers (16 bits; the second product is free beside the loads), accumulation and softmax state in
+// fp32.  f32: the same on the fp32 matrix instruction, without the turning.
+//
+// The work is cut by tokens, not by sequences: paged_plan.hpp.  Every workgroup finds its run in the running sum of the lengths (they are
+// on the device), and the pieces that are not a whole sequence are joined by a second kernel.
+#include <algorithm>
+#include <climits>
+#include "common.hpp"
+#include "paged_plan.hpp"
+
+namespace basa {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
+
+constexpr int kGroupsPerCu = 3, kCUs = 256;
+constexpr int kMaxDecodeGroups = kGroupsPerCu * kCUs;
+
+struct DecodeArgs {
+  const char *q, *k, *v;
+  int64_t q_b, q_h;                         // strides in bytes
+  int64_t k_b, k_h, k_l, v_b, v_h, v_l;
+  const int32_t *table, *lens;
+  int64_t table_stride;
+  int batch, heads_kv, group, units, pages; // units: runs of 16 kNT query heads that share a KV head
+  int64_t row_tokens;                       // tokens a table row has room for
+  FastDiv page;
+  char* out;
+  int64_t out_b, out_h;                     // in bytes
+  float* lse;                               // [batch][heads_q] or null
+  int groups;                               // workgroups
+  int64_t* first_tile;                      // workspace: [batch + 1], the last one the run's length
+  float* part_o;                            // [2 groups][16 kNT][d], not normalised
+  float2* part_ml;                          // [2 groups][16 kNT] maximum, sum
+  float scale, scale_log2e;
+};
+
+__device__ __forceinline__ int64_t cached_tokens(const DecodeArgs& a, int b) {
+  return min(max((int64_t)a.lens[b], (int64_t)0), a.row_tokens);
+}
+__device__ __forceinline__ float column_max(float v) {      // over the four lane groups
+  uint32_t x, y;
+  lane_pair<32>(__float_as_uint(v), x, y);
+  v = fmaxf(__uint_as_float(x), __uint_as_float(y));
+  lane_pair<16>(__float_as_uint(v), x, y);
+  return fmaxf(__uint_as_float(x), __uint_as_float(y));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  uint32_t x, y;
+  lane_pair<32>(__float_as_uint(v), x, y);
+  v = __uint_as_float(x) + __uint_as_float(y);
+  lane_pair<16>(__float_as_uint(v), x, y);
+  return __uint_as_float(x) + __uint_as_float(y);
+}
+// e^((s - m) / sqrt(d)) with m = -inf where nothing was seen yet
+__device__ __forceinline__ float weight_of(float s, float m, float scale_log2e) {
+  return __builtin_amdgcn_exp2f((s - (m == -INFINITY ? 0.f : m)) * scale_log2e);
+}
+__device__ __forceinline__ float lse_of(float m, float l, float scale) {
+  return l == 0.f ? -INFINITY : fmaf(m, scale, __logf(l));
+}
+template <bool kBf16>
+__device__ __forceinline__ void store4(char* at, floatx4 o) {
+  if constexpr (kBf16) {
+    bf16x4 t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) t[e] = (__bf16)o[e];
+    *reinterpret_cast<bf16x4*>(at) = t;
+  } else {
+    *reinterpret_cast<floatx4*>(at) = o;
+  }
+}
+
+template <bool kBf16, int kD, int kNT>
+__global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(DecodeArgs a) {
+  constexpr int kHeads = 16 * kNT, kElem = kBf16 ? 2 : 4;
+  constexpr int kKSteps = kD * kElem / 64;               // 16-byte chunks of a K row per lane
+  constexpr int kBlocks = kD / 16;                       // output blocks of 16 dimensions
+  constexpr int kVLoads = kBf16 ? 1 : kD / 64;           // loads of a V row per lane: kD / 16 numbers (bf16), 4 at a time (f32)
+  __shared__ int64_t row_at[kDecodeWaves][2][kDecodeTile];
+  __shared__ float part[kDecodeWaves][kHeads][kD + 4];
+  __shared__ float2 part_ml[kDecodeWaves][kHeads];
+  __shared__ int64_t wave_sum[4], found_first;
+  __shared__ int found;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
+
+  // the run of this workgroup and the sequence that its first tile is of
+  const int64_t per_tile = (int64_t)a.heads_kv * a.units;
+  const int each = (a.batch + 255) / 256, i0 = min(tid * each, a.batch), i1 = min(i0 + each, a.batch);
+  int64_t mine = 0;
+  for (int i = i0; i < i1; ++i) mine += decode_tiles(cached_tokens(a, i)) * per_tile;
+  int64_t x = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  if (lane == 63) wave_sum[wave] = x;
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  int64_t before = x - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) before += wave_sum[w];
+    total += wave_sum[w];
+  }
+  const int64_t run = decode_run(total, a.groups), begin = blockIdx.x * run, end = min(begin + run, total);
+  if (begin >= total) return;
+  if (before <= begin && begin < before + mine) {
+    int i = i0;
+    int64_t at = before;
+    for (;; ++i) {
+      const int64_t n = decode_tiles(cached_tokens(a, i)) * per_tile;
+      if (begin < at + n) break;
+      at += n;
+    }
+    found = i;
+    found_first = at;
+  }
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  int b = __builtin_amdgcn_readfirstlane(found);
+  int64_t first = found_first;
+  if (blockIdx.x == 0 && tid == 0) a.first_tile[a.batch] = run;
+
+  for (int64_t pos = begin; pos < end;) {
+    const int len = (int)cached_tokens(a, b), tiles = (int)decode_tiles(len);
+    const int unit = (int)((pos - first) / tiles), t0 = (int)(pos - first - (int64_t)unit * tiles);
+    const int t1 = (int)min((int64_t)tiles, t0 + (end - pos));
+    const int kvh = unit / a.units, h0 = kvh * a.group + (unit - kvh * a.units) * kHeads;
+    const int heads = min(kHeads, (kvh + 1) * a.group - h0);
+    if (unit == 0 && t0 == 0 && tid == 0) a.first_tile[b] = first;
+
+    // queries: lane (g, n) holds chunk 4 c + g of head n
+    uintx4 qf[kNT][kKSteps];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+      for (int c = 0; c < kKSteps; ++c) {
+        const int h = nt * 16 + r;
+        qf[nt][c] = *reinterpret_cast<const uintx4*>(a.q + b * a.q_b + (h0 + min(h, heads - 1)) * a.q_h + (4 * c + g) * 16);
+      }
+    floatx4 acc[kNT][kBlocks];
+    float m[kNT], l[kNT];
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      m[nt] = -INFINITY;
+      l[nt] = 0.f;
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) acc[nt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int32_t* table = a.table + (int64_t)b * a.table_stride;
+    const char* k_head = a.k + kvh * a.k_h;
+    const char* v_head = a.v + kvh * a.v_h;
+    const int64_t page_stride = lane < 32 ? a.k_b : a.v_b, row_stride = lane < 32 ? a.k_l : a.v_l;
+    int page_id = -1, page_off = 0;
+    auto look_up = [&](int t) {               // the page of the lane's token of tile t; both halves of the wave: the same tokens
+      const int64_t tok = (int64_t)t * kDecodeTile + (lane & 31);
+      page_id = -1;
+      if (t < t1 && tok < len) {
+        const int p = (int)a.page.div((uint32_t)tok);
+        page_off = (int)tok - p * (int)a.page.d;
+        page_id = table[p];
+      }
+    };
+    look_up(t0 + wave);
+    for (int t = t0 + wave; t < t1; t += kDecodeWaves) {
+      const bool valid = (unsigned)page_id < (unsigned)a.pages;
+      const uint32_t live = (uint32_t)__ballot(valid);
+      row_at[wave][lane >> 5][lane & 31] = valid ? page_id * page_stride + page_off * row_stride : 0;
+      look_up(t + kDecodeWaves);
+      uintx4 kf[2][kKSteps];
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const char* row = k_head + row_at[wave][0][16 * s + r] + g * 16;
+#pragma unroll
+        for (int c = 0; c < kKSteps; ++c) kf[s][c] = *reinterpret_cast<const uintx4*>(row + c * 64);
+      }
+      uint32_t vf[2][4][kVLoads][4];
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const char* row = v_head + row_at[wave][1][16 * s + 4 * g + j];
+#pragma unroll
+          for (int u = 0; u < kVLoads; ++u) {
+            if constexpr (kBf16 && kD == 64) {
+              const uintx2 w = *reinterpret_cast<const uintx2*>(row + r * 8);
+              vf[s][j][u][0] = w[0]; vf[s][j][u][1] = w[1];
+            } else {
+              const uintx4 w = *reinterpret_cast<const uintx4*>(row + r * 16 + u * 256);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) vf[s][j][u][e] = w[e];
+            }
+          }
+        }
+      floatx4 sc[kNT][2];
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          sc[nt][s] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int c = 0; c < kKSteps; ++c) {
+            if constexpr (kBf16) {
+              sc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[s][c]), __builtin_bit_cast(bf16x8, qf[nt][c]),
+                                                                  sc[nt][s], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                sc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[s][c][e]), __uint_as_float(qf[nt][c][e]), sc[nt][s],
+                                                                 0, 0, 0);
+            }
+          }
+        }
+      if (live != 0xffffffffu) {              // past the end, or a page that is none: no weight, whatever the rows hold
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const bool on = (live >> (16 * s + 4 * g + j)) & 1;
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) sc[nt][s][j] = on ? sc[nt][s][j] : -INFINITY;
+#pragma unroll
+            for (int u = 0; u < kVLoads; ++u)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) vf[s][j][u][e] = on ? vf[s][j][u][e] : 0u;
+          }
+      }
+      bf16x8 hi[kNT], lo[kNT];
+#pragma unroll
+      for (int nt = 0; nt < kNT; ++nt) {
+        float top = m[nt];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[nt][s][j]);
+        top = column_max(top);
+        const float old = weight_of(m[nt], top, a.scale_log2e);
+        m[nt] = top;
+        float sum = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float p = weight_of(sc[nt][s][j], top, a.scale_log2e);
+            sc[nt][s][j] = p;
+            sum += p;
+            if constexpr (kBf16) {
+              const __bf16 h = (__bf16)p;
+              hi[nt][4 * s + j] = h;
+              lo[nt][4 * s + j] = (__bf16)(p - (float)h);
+            }
+          }
+        l[nt] = fmaf(l[nt], old, sum);
+#pragma unroll
+        for (int e = 0; e < kBlocks; ++e) acc[nt][e] *= old;
+      }
+      if constexpr (kBf16) {
+#pragma unroll
+        for (int e = 0; e < kBlocks; ++e) {
+          // eight tokens of dimension kBlocks r + e
+          constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
+          uintx4 w;
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            w[j] = __builtin_amdgcn_perm(vf[j >> 1][2 * (j & 1) + 1][0][e >> 1], vf[j >> 1][2 * (j & 1)][0][e >> 1], e & 1 ? kHigh : kLow);
+#pragma unroll
+          for (int nt = 0; nt < kNT; ++nt) {
+            acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), hi[nt], acc[nt][e], 0, 0, 0);
+            acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), lo[nt], acc[nt][e], 0, 0, 0);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < kBlocks; ++e)
+#pragma unroll
+              for (int nt = 0; nt < kNT; ++nt)
+                acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[s][j][e >> 2][e & 3]), sc[nt][s][j], acc[nt][e], 0, 0, 0);
+      }
+    }
+
+    // the four waves together.  Block e, register i of lane (g, n): head n; dimension kBlocks (4 g + i) + e (bf16), 64 (e / 4) + 4 (4 g + i) +
+    // e % 4 (f32)
+#pragma unroll
+    for (int nt = 0; nt < kNT; ++nt) {
+      const int h = nt * 16 + r;
+      const float sum = column_sum(l[nt]);
+      if (h < heads) {
+        if (g == 0) part_ml[wave][h] = make_float2(m[nt], sum);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int e = 0; e < kBlocks; e += 4) {
+            const int dim = kBf16 ? kBlocks * (4 * g + i) + e : 16 * e + 4 * (4 * g + i);
+            *reinterpret_cast<floatx4*>(&part[wave][h][dim]) = floatx4{acc[nt][e][i], acc[nt][e + 1][i], acc[nt][e + 2][i], acc[nt][e + 3][i]};
+          }
+      }
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    const bool whole = t0 == 0 && t1 == tiles;
+    const int64_t place = decode_part(pos - t0 + 0, blockIdx.x, run);
+    for (int i = tid; i < heads * (kD / 4); i += 256) {
+      const int h = i / (kD / 4), c = i % (kD / 4);
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, part_ml[w][h].x);
+      floatx4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kDecodeWaves; ++w) {
+        const float2 ml = part_ml[w][h];
+        const float f = weight_of(ml.x, top, a.scale_log2e);
+        sum = fmaf(ml.y, f, sum);
+        o += *reinterpret_cast<const floatx4*>(&part[w][h][4 * c]) * f;
+      }
+      if (whole) {
+        store4<kBf16>(a.out + b * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
+        if (a.lse && c == 0) a.lse[(int64_t)b * a.heads_kv * a.group + h0 + h] = lse_of(top, sum, a.scale);
+      } else {
+        *reinterpret_cast<floatx4*>(a.part_o + (place * kHeads + h) * kD + 4 * c) = o;
+        if (c == 0) a.part_ml[place * kHeads + h] = make_float2(top, sum);
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    pos += t1 - t0;
+    if (t1 == tiles && unit + 1 == per_tile) {
+      ++b;
+      first = pos;
+    }
+  }
+}
+
+// The pieces of a (sequence, query head) that more than one workgroup had a part in, added up: a workgroup per sequence and head, 4 numbers to
+// a lane, every 256 / (d / 4)-th part to a lane group.
+template <bool kBf16, int kD>
+__global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int heads_per_unit) {
+  constexpr int kLanes = kD / 4, kRows = 256 / kLanes, kElem = kBf16 ? 2 : 4;
+  __shared__ floatx4 row_o[kRows][kLanes];
+  __shared__ float2 row_ml[kRows];
+  const int heads_q = a.heads_kv * a.group, b = blockIdx.x / heads_q, head = blockIdx.x - b * heads_q;
+  const int kvh = head / a.group, sub = (head - kvh * a.group) / heads_per_unit, h = head - kvh * a.group - sub * heads_per_unit;
+  const int64_t run = a.first_tile[a.batch], tiles = decode_tiles(cached_tokens(a, b));
+  const int64_t first = a.first_tile[b] + (int64_t)(kvh * a.units + sub) * tiles;
+  const int g0 = (int)(first / run), g1 = (int)((first + tiles - 1) / run);
+  if (g0 == g1) return;
+  const int c = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
+  float m = -INFINITY, l = 0.f;
+  floatx4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int w = g0 + row; w <= g1; w += kRows) {
+    const int64_t place = (int64_t)decode_part(first, w, run) * heads_per_unit + h;
+    const float2 ml = a.part_ml[place];
+    const floatx4 p = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
+    const float top = fmaxf(m, ml.x), f0 = weight_of(m, top, a.scale_log2e), f1 = weight_of(ml.x, top, a.scale_log2e);
+    m = top;
+    l = l * f0 + ml.y * f1;
+    o = o * f0 + p * f1;
+  }
+  row_o[row][c] = o;
+  if (c == 0) row_ml[row] = make_float2(m, l);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  if (row > 0) return;
+  float top = -INFINITY, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) top = fmaxf(top, row_ml[i].x);
+  o = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kRows; ++i) {
+    const float f = weight_of(row_ml[i].x, top, a.scale_log2e);
+    sum = fmaf(row_ml[i].y, f, sum);
+    o += row_o[i][c] * f;
+  }
+  store4<kBf16>(a.out + b * a.out_b + head * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
+  if (a.lse && c == 0) a.lse[blockIdx.x] = lse_of(top, sum, a.scale);
+}
+
+// Query heads that share the loads of their KV head: up to 32 (bf16), 16 (f32, whose rows take twice the registers).
+int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
+int decode_groups(int batch, int heads_kv, int group, bool bf16, int64_t row_tokens) {
+  const int hpu = heads_per_unit(group, bf16);
+  const int64_t most = (int64_t)batch * heads_kv * ceil_div(group, hpu) * decode_tiles(row_tokens);
+  return (int)std::min<int64_t>(kMaxDecodeGroups, (most + kDecodeWaves - 1) / kDecodeWaves);
+}
+struct DecodeWs { size_t first_tile, part_o, part_ml, total; };
+DecodeWs carve(int batch, int groups, int hpu, int d) {
+  DecodeWs w;
+  size_t o = 0;
+  w.first_tile = o; o += align_up((size_t)(batch + 1) * 8, 256);
+  w.part_o = o; o += align_up((size_t)2 * groups * hpu * d * 4, 256);
+  w.part_ml = o; o += align_up((size_t)2 * groups * hpu * 8, 256);
+  w.total = o;
+  return w;
+}
+
+template <bool kBf16, int kD, int kNT>
+basa_status launch(const DecodeArgs& a, hipStream_t st) {
+  {
+    ProfScope prof(K_DECODE, st);
+    decode_kernel<kBf16, kD, kNT><<<a.groups, 256, 0, st>>>(a);
+    BASA_HIP_CHECK_LAUNCH("decode_kernel");
+  }
+  if (a.groups == 1) return BASA_OK;
+  ProfScope prof(K_DECODE_JOIN, st);
+  decode_join_kernel<kBf16, kD><<<a.batch * a.heads_kv * a.group, 256, 0, st>>>(a, 16 * kNT);
+  BASA_HIP_CHECK_LAUNCH("decode_join_kernel");
+  return BASA_OK;
+}
+
+}  // namespace
+
+size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int64_t row_tokens) {
+  const int group = heads_q / heads_kv;
+  return carve(batch, decode_groups(batch, heads_kv, group, bf16, row_tokens), heads_per_unit(group, bf16), d).total;
+}
+
+basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
+                               int64_t table_stride, const int32_t* lens, void* out, int64_t out_sb, int64_t out_sh, float* lse, void* ws,
+                               hipStream_t st) {
+  DecodeArgs a{};
+  const bool bf16 = q.dtype == BASA_BF16;
+  const int e = bf16 ? 2 : 4;
+  a.q = static_cast<const char*>(q.ptr); a.k = static_cast<const char*>(k_pages.ptr); a.v = static_cast<const char*>(v_pages.ptr);
+  a.q_b = q.stride_b * e; a.q_h = q.stride_h * e;
+  a.k_b = k_pages.stride_b * e; a.k_h = k_pages.stride_h * e; a.k_l = k_pages.stride_l * e;
+  a.v_b = v_pages.stride_b * e; a.v_h = v_pages.stride_h * e; a.v_l = v_pages.stride_l * e;
+  a.table = table; a.table_stride = table_stride; a.lens = lens;
+  a.batch = q.batch; a.heads_kv = k_pages.heads; a.group = q.heads / k_pages.heads; a.pages = k_pages.batch;
+  a.row_tokens = (int64_t)width * k_pages.L;
+  a.page = fast_div((uint32_t)k_pages.L);
+  const int hpu = heads_per_unit(a.group, bf16);
+  a.units = ceil_div(a.group, hpu);
+  a.out = static_cast<char*>(out); a.out_b = out_sb * e; a.out_h = out_sh * e; a.lse = lse;
+  a.groups = decode_groups(a.batch, a.heads_kv, a.group, bf16, a.row_tokens);
+  const DecodeWs w = carve(a.batch, a.groups, hpu, q.d);
+  char* base = static_cast<char*>(ws);
+  a.first_tile = reinterpret_cast<int64_t*>(base + w.first_tile);
+  a.part_o = reinterpret_cast<float*>(base + w.part_o);
+  a.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
+  a.scale = 1.0f / sqrtf((float)q.d);
+  a.scale_log2e = 1.4426950408889634f / sqrtf((float)q.d);
+  if (!bf16) return q.d == 128 ? launch<false, 128, 1>(a, st) : launch<false, 64, 1>(a, st);
+  if (hpu == 16) return q.d == 128 ? launch<true, 128, 1>(a, st) : launch<true, 64, 1>(a, st);
+  return q.d == 128 ? launch<true, 128, 2>(a, st) : launch<true, 64, 2>(a, st);
+}
+
+}  // namespace basa

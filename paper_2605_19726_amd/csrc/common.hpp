@@ -42,7 +42,7 @@ basa_status hip_fail(hipError_t e, const char* what);
 // with a pair of HIP events on the launch stream when profiling is enabled.
 enum KernelId {
   K_NORM_TILE_SORT = 0, K_MERGE, K_STATS, K_SCORES, K_ROW_SELECT, K_GATHER, K_ATTN,
-  K_ATTN_F32, K_BLOCK_MASS, K_DIAG_SMALL, K_SCORES_SELECT, K_ATTN_COMBINE, K_COUNT
+  K_ATTN_F32, K_BLOCK_MASS, K_DIAG_SMALL, K_SCORES_SELECT, K_ATTN_COMBINE, K_PAGED, K_DECODE, K_DECODE_JOIN, K_COUNT
 };
 struct ProfScope {
   ProfScope(int id, hipStream_t st);
@@ -175,6 +175,20 @@ basa_status launch_attn_f32(const AttnArgs& a, hipStream_t st);
 // their (running maximum in log2 units, sum) part_ml[split][BHq][Lq], rows by sorted position.
 basa_status launch_attn_combine(const AttnArgs& a, const float* part_o, const float2* part_ml, int splits, hipStream_t st);
 basa_status launch_attn_mfma(const AttnArgs& a, hipStream_t st);
+
+// Paged key-value cache (paged.hip) and the attention of single tokens over it (attn_decode.hip).  Pages are [pages, heads, page, d] views.
+bool page_tables_take(int n_seq);
+basa_status launch_page_tables(const int32_t* have, const int32_t* add, int n, int page, int32_t* table, int width, int64_t table_stride,
+                               const int32_t* free_pages, int n_free, int64_t* slots, int tokens, int32_t* lens, int32_t* cu,
+                               int32_t* pages, hipStream_t st);
+basa_status launch_cache_append(const TensorView& k, const TensorView& v, const int64_t* slots, const TensorView& k_pages,
+                                const TensorView& v_pages, hipStream_t st);
+basa_status launch_cache_gather(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
+                                int64_t table_stride, const int32_t* cu, int n, const TensorView& k, const TensorView& v, hipStream_t st);
+size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int64_t row_tokens);
+basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
+                               int64_t table_stride, const int32_t* lens, void* out, int64_t out_sb, int64_t out_sh, float* lse, void* ws,
+                               hipStream_t st);
 
 // Selection-fidelity diagnostics (diag.hip).  block mass: bf16 on the matrix cores, f32 on a plain kernel.
 size_t block_mass_workspace_bytes(int BHq, int BHkv, int Lq, int Lk, int d);
