@@ -5,8 +5,10 @@
 // running maximum and sum per query head.  4 group flops for 2 bytes of bf16: bound by the memory up to a group of several hundred, so that
 // everything serves the loads: the matrix instruction takes the query heads of a KV head as its 16 columns, used or not.
 //
-// Operands straight from memory, no LDS in between.  A wave takes 32 tokens at a time.  S^T = K Q^T: lane (g, r) of the A operand
-// holds 16 bytes of token r, chunk 4 c + g of its row at step c; the queries are laid out alike.  Of the result, lane (g, n) holds tokens
+// Operands straight from memory, no LDS in between.  A wave takes 32 tokens at a time, in two halves of 16.  S^T = K Q^T: lane (g, r) of the
+// A operand holds 16 bytes of token r, chunk 4 c + g of its row at step c; the queries are laid out alike.  Loaded like that an instruction
+// would take half a line of 128 bytes from each of 16 rows; so two steps are loaded together, whole lines of 8 rows by each
+// instruction, and lanes r and r ^ 8 exchange one of their two chunks in registers.  Of the result, lane (g, n) holds tokens
 // 4 g .. 4 g + 3 of each half for query head n: as they are, the B operand of O^T += V^T P^T, if token order within the sum is that
 // of lane group g: its own eight tokens.  The A operand is eight tokens of one dimension: lane (g, r) loads its group's eight
 // tokens, chunk r of each row (whole rows, 16 lanes of 16 bytes), and turns its 8 x 8 block in registers, a byte permutation for two
@@ -30,9 +32,6 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t uintx2 __attribute__((ext_vector_type(2)));
 
-constexpr int kGroupsPerCu = 3, kCUs = 256;
-constexpr int kMaxDecodeGroups = kGroupsPerCu * kCUs;
-
 struct DecodeArgs {
   const char *q, *k, *v;
   int64_t q_b, q_h;                         // strides in bytes
@@ -46,9 +45,10 @@ struct DecodeArgs {
   int64_t out_b, out_h;                     // in bytes
   float* lse;                               // [batch][heads_q] or null
   int groups;                               // workgroups
-  int64_t* first_tile;                      // workspace: [batch + 1], the last one the run's length
-  float* part_o;                            // [2 groups][16 kNT][d], not normalised
-  float2* part_ml;                          // [2 groups][16 kNT] maximum, sum
+  int64_t* first_place;                     // workspace: [batch + 1], the last one the length of a run
+  int part_heads;                           // query heads of a partial result
+  float* part_o;                            // [2 groups][part_heads][d], not normalised
+  float2* part_ml;                          // [2 groups][part_heads] maximum, sum
   float scale, scale_log2e;
 };
 
@@ -76,6 +76,10 @@ __device__ __forceinline__ float weight_of(float s, float m, float scale_log2e) 
 __device__ __forceinline__ float lse_of(float m, float l, float scale) {
   return l == 0.f ? -INFINITY : fmaf(m, scale, __logf(l));
 }
+// The cache is read once: its lines are the first to leave the L2.  (Pays only where an instruction takes whole lines of 128 bytes; with half
+// lines, whose other half is asked for by the next instruction, they leave before that.)
+template <class T>
+__device__ __forceinline__ T load_once(const char* at) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(at)); }
 template <bool kBf16>
 __device__ __forceinline__ void store4(char* at, floatx4 o) {
   if constexpr (kBf16) {
@@ -89,7 +93,7 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
 }
 
 template <bool kBf16, int kD, int kNT>
-__global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(DecodeArgs a) {
+__global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
   constexpr int kHeads = 16 * kNT, kElem = kBf16 ? 2 : 4;
   constexpr int kKSteps = kD * kElem / 64;               // 16-byte chunks of a K row per lane
   constexpr int kBlocks = kD / 16;                       // output blocks of 16 dimensions
@@ -101,11 +105,11 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
   __shared__ int found;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
 
-  // the run of this workgroup and the sequence that its first tile is of
-  const int64_t per_tile = (int64_t)a.heads_kv * a.units;
+  // the run of this workgroup and the sequence that its first place is of
+  const int64_t per_seq = (int64_t)a.heads_kv * a.units;
   const int each = (a.batch + 255) / 256, i0 = min(tid * each, a.batch), i1 = min(i0 + each, a.batch);
   int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += decode_tiles(cached_tokens(a, i)) * per_tile;
+  for (int i = i0; i < i1; ++i) mine += decode_places(cached_tokens(a, i)) * per_seq;
   int64_t x = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -121,13 +125,13 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
     if (w < wave) before += wave_sum[w];
     total += wave_sum[w];
   }
-  const int64_t run = decode_run(total, a.groups), begin = blockIdx.x * run, end = min(begin + run, total);
+  const int64_t run = decode_run(total), begin = blockIdx.x * run, end = min(begin + run, total);
   if (begin >= total) return;
   if (before <= begin && begin < before + mine) {
     int i = i0;
     int64_t at = before;
     for (;; ++i) {
-      const int64_t n = decode_tiles(cached_tokens(a, i)) * per_tile;
+      const int64_t n = decode_places(cached_tokens(a, i)) * per_seq;
       if (begin < at + n) break;
       at += n;
     }
@@ -138,15 +142,24 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
   __syncthreads();
   int b = __builtin_amdgcn_readfirstlane(found);
   int64_t first = found_first;
-  if (blockIdx.x == 0 && tid == 0) a.first_tile[a.batch] = run;
+  if (blockIdx.x == 0 && tid == 0) a.first_place[a.batch] = run;
 
   for (int64_t pos = begin; pos < end;) {
-    const int len = (int)cached_tokens(a, b), tiles = (int)decode_tiles(len);
-    const int unit = (int)((pos - first) / tiles), t0 = (int)(pos - first - (int64_t)unit * tiles);
-    const int t1 = (int)min((int64_t)tiles, t0 + (end - pos));
+    const int len = (int)cached_tokens(a, b), steps = (int)decode_steps(len);
+    const int unit = (int)((pos - first) / (steps + kDecodeLead));
+    const int64_t seq_first = first, head_first = first + (int64_t)unit * (steps + kDecodeLead);
+    const DecodePiece piece = decode_piece(head_first, steps, blockIdx.x, run);
+    const int seq = b;
+    pos = head_first + steps + kDecodeLead;
+    if (unit + 1 == per_seq) {
+      ++b;
+      first = pos;
+    }
+    if (piece.t1 <= piece.t0) continue;      // the run ends before its first step
+    const int t0 = (int)piece.t0 * kDecodeWaves, t1 = min((int)piece.t1 * kDecodeWaves, (len + kDecodeTile - 1) / kDecodeTile);   // tiles
     const int kvh = unit / a.units, h0 = kvh * a.group + (unit - kvh * a.units) * kHeads;
     const int heads = min(kHeads, (kvh + 1) * a.group - h0);
-    if (unit == 0 && t0 == 0 && tid == 0) a.first_tile[b] = first;
+    if (unit == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
 
     // queries: lane (g, n) holds chunk 4 c + g of head n
     uintx4 qf[kNT][kKSteps];
@@ -155,7 +168,7 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
 #pragma unroll
       for (int c = 0; c < kKSteps; ++c) {
         const int h = nt * 16 + r;
-        qf[nt][c] = *reinterpret_cast<const uintx4*>(a.q + b * a.q_b + (h0 + min(h, heads - 1)) * a.q_h + (4 * c + g) * 16);
+        qf[nt][c] = *reinterpret_cast<const uintx4*>(a.q + seq * a.q_b + (h0 + min(h, heads - 1)) * a.q_h + (4 * c + g) * 16);
       }
     floatx4 acc[kNT][kBlocks];
     float m[kNT], l[kNT];
@@ -166,7 +179,7 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
 #pragma unroll
       for (int e = 0; e < kBlocks; ++e) acc[nt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const int32_t* table = a.table + (int64_t)b * a.table_stride;
+    const int32_t* table = a.table + (int64_t)seq * a.table_stride;
     const char* k_head = a.k + kvh * a.k_h;
     const char* v_head = a.v + kvh * a.v_h;
     const int64_t page_stride = lane < 32 ? a.k_b : a.v_b, row_stride = lane < 32 ? a.k_l : a.v_l;
@@ -188,11 +201,13 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
       look_up(t + kDecodeWaves);
       uintx4 kf[2][kKSteps];
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const char* row = k_head + row_at[wave][0][16 * s + r] + g * 16;
+      for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int c = 0; c < kKSteps; ++c) kf[s][c] = *reinterpret_cast<const uintx4*>(row + c * 64);
-      }
+        for (int i = 0; i < 2; ++i) {         // rows 8 i .. 8 i + 7 of the half, a line of 128 bytes each
+          const char* row = k_head + row_at[wave][0][16 * s + 8 * i + (r & 7)] + (r >> 3) * 64 + g * 16;
+#pragma unroll
+          for (int c = 0; c < kKSteps; c += 2) kf[s][c + i] = load_once<uintx4>(row + c * 64);
+        }
       uint32_t vf[2][4][kVLoads][4];
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -202,15 +217,25 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
 #pragma unroll
           for (int u = 0; u < kVLoads; ++u) {
             if constexpr (kBf16 && kD == 64) {
-              const uintx2 w = *reinterpret_cast<const uintx2*>(row + r * 8);
+              const uintx2 w = load_once<uintx2>(row + r * 8);
               vf[s][j][u][0] = w[0]; vf[s][j][u][1] = w[1];
             } else {
-              const uintx4 w = *reinterpret_cast<const uintx4*>(row + r * 16 + u * 256);
+              const uintx4 w = load_once<uintx4>(row + r * 16 + u * 256);
 #pragma unroll
               for (int e = 0; e < 4; ++e) vf[s][j][u][e] = w[e];
             }
           }
         }
+#pragma unroll
+      for (int s = 0; s < 2; ++s)             // lanes r < 8 want both chunks of the first rows, the others both of the second
+#pragma unroll
+        for (int c = 0; c < kKSteps; c += 2)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = kf[s][c][e], y = kf[s][c + 1][e], other = lane_xor<8>(r < 8 ? y : x);
+            kf[s][c][e] = r < 8 ? x : other;
+            kf[s][c + 1][e] = r < 8 ? other : y;
+          }
       floatx4 sc[kNT][2];
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
@@ -320,8 +345,8 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    const bool whole = t0 == 0 && t1 == tiles;
-    const int64_t place = decode_part(pos - t0 + 0, blockIdx.x, run);
+    const bool whole = piece.t0 == 0 && piece.t1 == steps;
+    const int64_t place = decode_part(piece, blockIdx.x) * a.part_heads;
     for (int i = tid; i < heads * (kD / 4); i += 256) {
       const int h = i / (kD / 4), c = i % (kD / 4);
       float top = -INFINITY, sum = 0.f;
@@ -336,25 +361,21 @@ __global__ __launch_bounds__(256, kNT == 1 && kBf16 ? 3 : 2) void decode_kernel(
         o += *reinterpret_cast<const floatx4*>(&part[w][h][4 * c]) * f;
       }
       if (whole) {
-        store4<kBf16>(a.out + b * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
-        if (a.lse && c == 0) a.lse[(int64_t)b * a.heads_kv * a.group + h0 + h] = lse_of(top, sum, a.scale);
+        store4<kBf16>(a.out + seq * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
+        if (a.lse && c == 0) a.lse[(int64_t)seq * a.heads_kv * a.group + h0 + h] = lse_of(top, sum, a.scale);
       } else {
-        *reinterpret_cast<floatx4*>(a.part_o + (place * kHeads + h) * kD + 4 * c) = o;
-        if (c == 0) a.part_ml[place * kHeads + h] = make_float2(top, sum);
+        *reinterpret_cast<floatx4*>(a.part_o + (place + h) * kD + 4 * c) = o;
+        if (c == 0) a.part_ml[place + h] = make_float2(top, sum);
       }
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    pos += t1 - t0;
-    if (t1 == tiles && unit + 1 == per_tile) {
-      ++b;
-      first = pos;
-    }
   }
 }
 
 // The pieces of a (sequence, query head) that more than one workgroup had a part in, added up: a workgroup per sequence and head, 4 numbers to
-// a lane, every 256 / (d / 4)-th part to a lane group.
+// a lane, every 256 / (d / 4)-th part to a lane group, four of them requested at once.
+constexpr int kPartsAtOnce = 4;
 template <bool kBf16, int kD>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int heads_per_unit) {
   constexpr int kLanes = kD / 4, kRows = 256 / kLanes, kElem = kBf16 ? 2 : 4;
@@ -362,21 +383,37 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
   __shared__ float2 row_ml[kRows];
   const int heads_q = a.heads_kv * a.group, b = blockIdx.x / heads_q, head = blockIdx.x - b * heads_q;
   const int kvh = head / a.group, sub = (head - kvh * a.group) / heads_per_unit, h = head - kvh * a.group - sub * heads_per_unit;
-  const int64_t run = a.first_tile[a.batch], tiles = decode_tiles(cached_tokens(a, b));
-  const int64_t first = a.first_tile[b] + (int64_t)(kvh * a.units + sub) * tiles;
-  const int g0 = (int)(first / run), g1 = (int)((first + tiles - 1) / run);
+  const int64_t run = a.first_place[a.batch], steps = decode_steps(cached_tokens(a, b));
+  const int64_t first = a.first_place[b] + (int64_t)(kvh * a.units + sub) * (steps + kDecodeLead);
+  const int g0 = (int)decode_first_group(first, run), g1 = (int)decode_last_group(first, steps, run);
   if (g0 == g1) return;
   const int c = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
   float m = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int w = g0 + row; w <= g1; w += kRows) {
-    const int64_t place = (int64_t)decode_part(first, w, run) * heads_per_unit + h;
-    const float2 ml = a.part_ml[place];
-    const floatx4 p = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
-    const float top = fmaxf(m, ml.x), f0 = weight_of(m, top, a.scale_log2e), f1 = weight_of(ml.x, top, a.scale_log2e);
+  for (int w0 = g0 + row; w0 <= g1; w0 += kRows * kPartsAtOnce) {
+    float2 ml[kPartsAtOnce];
+    floatx4 p[kPartsAtOnce];
+#pragma unroll
+    for (int j = 0; j < kPartsAtOnce; ++j) {
+      const int w = min(w0 + j * kRows, g1);
+      const int64_t place = decode_part(decode_piece(first, steps, w, run), w) * a.part_heads + h;
+      ml[j] = a.part_ml[place];
+      p[j] = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < kPartsAtOnce; ++j) top = fmaxf(top, ml[j].x);
+    const float old = weight_of(m, top, a.scale_log2e);
     m = top;
-    l = l * f0 + ml.y * f1;
-    o = o * f0 + p * f1;
+    l *= old;
+    o *= old;
+#pragma unroll
+    for (int j = 0; j < kPartsAtOnce; ++j) {
+      if (w0 + j * kRows > g1) break;
+      const float f = weight_of(ml[j].x, top, a.scale_log2e);
+      l = fmaf(ml[j].y, f, l);
+      o += p[j] * f;
+    }
   }
   row_o[row][c] = o;
   if (c == 0) row_ml[row] = make_float2(m, l);
@@ -399,18 +436,16 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
 
 // Query heads that share the loads of their KV head: up to 32 (bf16), 16 (f32, whose rows take twice the registers).
 int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
-int decode_groups(int batch, int heads_kv, int group, bool bf16, int64_t row_tokens) {
-  const int hpu = heads_per_unit(group, bf16);
-  const int64_t most = (int64_t)batch * heads_kv * ceil_div(group, hpu) * decode_tiles(row_tokens);
-  return (int)std::min<int64_t>(kMaxDecodeGroups, (most + kDecodeWaves - 1) / kDecodeWaves);
+int most_groups(int batch, int heads_kv, int group, bool bf16, int64_t row_tokens) {
+  return decode_groups((int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens));
 }
-struct DecodeWs { size_t first_tile, part_o, part_ml, total; };
-DecodeWs carve(int batch, int groups, int hpu, int d) {
+struct DecodeWs { size_t first_place, part_o, part_ml, total; };
+DecodeWs carve(int batch, int groups, int part_heads, int d) {
   DecodeWs w;
   size_t o = 0;
-  w.first_tile = o; o += align_up((size_t)(batch + 1) * 8, 256);
-  w.part_o = o; o += align_up((size_t)2 * groups * hpu * d * 4, 256);
-  w.part_ml = o; o += align_up((size_t)2 * groups * hpu * 8, 256);
+  w.first_place = o; o += align_up((size_t)(batch + 1) * 8, 256);
+  w.part_o = o; o += align_up((size_t)2 * groups * part_heads * d * 4, 256);
+  w.part_ml = o; o += align_up((size_t)2 * groups * part_heads * 8, 256);
   w.total = o;
   return w;
 }
@@ -422,7 +457,7 @@ basa_status launch(const DecodeArgs& a, hipStream_t st) {
     decode_kernel<kBf16, kD, kNT><<<a.groups, 256, 0, st>>>(a);
     BASA_HIP_CHECK_LAUNCH("decode_kernel");
   }
-  if (a.groups == 1) return BASA_OK;
+  if (a.row_tokens <= kDecodeStep) return BASA_OK;        // nothing to split
   ProfScope prof(K_DECODE_JOIN, st);
   decode_join_kernel<kBf16, kD><<<a.batch * a.heads_kv * a.group, 256, 0, st>>>(a, 16 * kNT);
   BASA_HIP_CHECK_LAUNCH("decode_join_kernel");
@@ -433,7 +468,7 @@ basa_status launch(const DecodeArgs& a, hipStream_t st) {
 
 size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int64_t row_tokens) {
   const int group = heads_q / heads_kv;
-  return carve(batch, decode_groups(batch, heads_kv, group, bf16, row_tokens), heads_per_unit(group, bf16), d).total;
+  return carve(batch, most_groups(batch, heads_kv, group, bf16, row_tokens), std::min(group, heads_per_unit(group, bf16)), d).total;
 }
 
 basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
@@ -453,10 +488,11 @@ basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, c
   const int hpu = heads_per_unit(a.group, bf16);
   a.units = ceil_div(a.group, hpu);
   a.out = static_cast<char*>(out); a.out_b = out_sb * e; a.out_h = out_sh * e; a.lse = lse;
-  a.groups = decode_groups(a.batch, a.heads_kv, a.group, bf16, a.row_tokens);
-  const DecodeWs w = carve(a.batch, a.groups, hpu, q.d);
+  a.groups = most_groups(a.batch, a.heads_kv, a.group, bf16, a.row_tokens);
+  a.part_heads = std::min(a.group, hpu);
+  const DecodeWs w = carve(a.batch, a.groups, a.part_heads, q.d);
   char* base = static_cast<char*>(ws);
-  a.first_tile = reinterpret_cast<int64_t*>(base + w.first_tile);
+  a.first_place = reinterpret_cast<int64_t*>(base + w.first_place);
   a.part_o = reinterpret_cast<float*>(base + w.part_o);
   a.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   a.scale = 1.0f / sqrtf((float)q.d);

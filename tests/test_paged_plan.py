@@ -16,9 +16,17 @@ int main() {
   long long a, b, c;
   while (std::scanf("%15s %lld %lld %lld", what, &a, &b, &c) == 4) {
     if (!std::strcmp(what, "div")) std::printf("%u\n", basa::fast_div((uint32_t)b).div((uint32_t)a));
-    if (!std::strcmp(what, "run")) std::printf("%lld\n", (long long)basa::decode_run(a, (int)b));
-    if (!std::strcmp(what, "tiles")) std::printf("%lld\n", (long long)basa::decode_tiles(a));
-    if (!std::strcmp(what, "part")) std::printf("%d\n", basa::decode_part(a, b, c));
+    if (!std::strcmp(what, "run")) std::printf("%lld\n", (long long)basa::decode_run(a));
+    if (!std::strcmp(what, "steps")) std::printf("%lld\n", (long long)basa::decode_steps(a));
+    if (!std::strcmp(what, "groups")) std::printf("%lld\n", (long long)basa::decode_groups(a));
+    if (!std::strcmp(what, "first")) std::printf("%lld\n", (long long)basa::decode_first_group(a, b));
+    if (!std::strcmp(what, "last")) std::printf("%lld\n", (long long)basa::decode_last_group(a, b, c));
+    if (!std::strcmp(what, "piece")) {          // a: first place, b: steps, c: group, d: run
+      long long d;
+      if (std::scanf("%lld", &d) != 1) return 1;
+      const basa::DecodePiece p = basa::decode_piece(a, b, c, d);
+      std::printf("%lld %lld %lld\n", (long long)p.t0, (long long)p.t1, (long long)basa::decode_part(p, c));
+    }
   }
 }
 """
@@ -31,7 +39,7 @@ def plan(tmp_path_factory):
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", build.CSRC, str(d / "p.cpp"), "-o", str(d / "p")], check=True)
 
     def call(questions):
-        text = "\n".join("%s %d %d %d" % tuple((list(q) + [0, 0])[:4]) for q in questions)
+        text = "\n".join("%s %d %d %d" % tuple((list(q) + [0, 0])[:4]) + (" %d" % q[4] if len(q) > 4 else "") for q in questions)
         return [int(x) for x in subprocess.run([str(d / "p")], input=text, check=True, capture_output=True, text=True).stdout.split()]
     return call
 
@@ -45,21 +53,36 @@ def test_division_by_a_page_size(plan):
     assert plan(asked) == [n // d for _, n, d in asked]
 
 
-def test_runs_cover_all_tiles_and_give_every_piece_a_place_of_its_own(plan):
+def test_runs_take_every_step_once_and_give_every_piece_a_place_of_its_own(plan):
     rng = random.Random(2)
-    for _ in range(60):
-        groups = rng.choice([1, 2, 5, 64, 768])
-        lens = [int(2 ** rng.uniform(0, 14)) - 1 for _ in range(rng.randint(1, 40))]
-        tiles = plan([("tiles", n) for n in lens])
-        assert tiles == [max(1, -(-n // 32)) for n in lens]
-        total = sum(tiles)
-        run, = plan([("run", total, groups)])
-        assert run % 4 == 0 and run * groups >= total and (run - 4) * groups < total
-        first, places, questions = 0, set(), []
-        for t in tiles:
-            g0, g1 = first // run, (first + t - 1) // run
-            if g0 != g1:
-                questions += [("part", first, g, run) for g in range(g0, g1 + 1)]
-            first += t
+    for case in range(80):
+        n, most = rng.randint(1, 60), rng.choice([7, 12, 16, 20])
+        lens = [int(2 ** rng.uniform(0, most)) - 1 for _ in range(n)]
+        steps = plan([("steps", x) for x in lens])
+        assert steps == [max(1, -(-x // 128)) for x in lens]
+        total = sum(steps) + n                                   # a place in front of every sequence
+        run, groups = plan([("run", total), ("groups", total)])
+        assert run >= 1 and run * groups >= total                # the launch has a group for every run
+        first, asked = 0, []
+        for t in steps:
+            asked += [("first", first, run), ("last", first, t, run)]
+            first += t + 1
+        ends, first, questions, of = plan(asked), 0, [], []
+        for i, t in enumerate(steps):
+            g0, g1 = ends[2 * i], ends[2 * i + 1]
+            for g in range(max(g0 - 1, 0), min(g1 + 1, groups - 1) + 1):
+                questions.append(("piece", first, t, g, run))
+                of.append((i, g, g0 <= g <= g1))
+            first += t + 1
         got = plan(questions)
-        assert len(set(got)) == len(got) and all(0 <= p < 2 * groups and p // 2 == q[2] for p, q in zip(got, questions))
+        done, places = [0] * n, set()
+        for (i, g, inside), t0, t1, place in zip(of, got[::3], got[1::3], got[2::3]):
+            assert (t1 > t0) == inside                           # the groups between first and last, and no others, have steps of it
+            if not inside:
+                continue
+            assert t0 == done[i]                                 # in order, without a gap
+            done[i] = t1
+            if (t0, t1) != (0, steps[i]):
+                assert place not in places and place // 2 == g < groups
+                places.add(place)
+        assert done == steps
