@@ -7,7 +7,6 @@ loaded the first call raises: there is no fallback.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
 import os
 from typing import Optional
@@ -186,7 +185,8 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(x: torch.Tensor):
-    return torch.cuda.current_stream(x.device).cuda_stream
+    # (the handle of torch.cuda.current_stream(x.device) without the Stream object, which costs 2 us a call)
+    return torch._C._cuda_getCurrentRawStream(x.device.index)
 
 
 def _ws(nbytes: int, device) -> torch.Tensor:
@@ -462,18 +462,24 @@ def _block_table(table: torch.Tensor, n_seq: int, device):
 
 def _packed_desc(x: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
     """Descriptor of packed rows [T, heads_kv, d] that belong to a cache."""
-    if x.dim() != 3 or x.shape[1] != cache.heads or x.shape[2] != cache.d or x.dtype != cache.dtype or x.device != cache.device:
-        raise ValueError(f"{name} must be a {cache.dtype} tensor [tokens, {cache.heads}, {cache.d}] on {cache.device}")
-    if x.stride(2) != 1:
+    shape, h, d = x.shape, cache.heads, cache.d
+    if len(shape) != 3 or shape[1] != h or shape[2] != d or x.dtype != cache.dtype or x.device != cache.device:
+        raise ValueError(f"{name} must be a {cache.dtype} tensor [tokens, {h}, {d}] on {cache.device}")
+    T, (st, sh, sd) = shape[0], x.stride()
+    if sd != 1:
         raise ValueError(f"{name}: the head dimension must be contiguous")
-    T, h, d = x.shape
-    st, sh = x.stride(0) if T > 1 else max(d, x.stride(0)), x.stride(1)
-    return BasaTensor(x.data_ptr(), _DTYPES[x.dtype], 1, h, T, d, 0, sh if h > 1 else 0, st)
+    return BasaTensor(x.data_ptr(), cache._kd.dtype, 1, h, T, d, 0, sh if h > 1 else 0, st if T > 1 else max(d, st))
 
 
-def _on_device(device):
-    """The device of a call's tensors as the current one, which its stream and its launches belong to."""
-    return contextlib.nullcontext() if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _launch(entry, x: torch.Tensor, *args):
+    """A library call on the current stream of x's device, with that device as the current one (its launches go there)."""
+    if x.device.index == torch.cuda.current_device():
+        status = entry(*args, _stream(x))
+    else:
+        with torch.cuda.device(x.device):
+            status = entry(*args, _stream(x))
+    if status != BASA_OK:
+        _check(status)
 
 
 def basa_page_tables(have, add, table, free_pages, page: int, tokens: int, out: Optional[PageTables] = None) -> PageTables:
@@ -488,8 +494,7 @@ def basa_page_tables(have, add, table, free_pages, page: int, tokens: int, out: 
             _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0],
             _int_array(out.slots, "slots", dev, (int(tokens),), torch.int64), int(tokens), _int_array(out.lens, "lens", dev, one),
             _int_array(out.cu, "cu", dev, (n + 1,)), _int_array(out.pages, "pages", dev, (2,)))
-    with _on_device(dev):
-        _check(lib.basa_page_tables(*args, _stream(table)))
+    _launch(lib.basa_page_tables, table, *args)
     return out
 
 
@@ -501,8 +506,7 @@ def basa_cache_append(k, v, slots, cache: PagedCache):
     at = _int_array(slots, "slots", cache.device, k.shape[:1], torch.int64)
     if k.shape[0] == 0:
         return
-    with _on_device(cache.device):
-        _check(load().basa_cache_append(C.byref(kd), C.byref(vd), at, *cache._keys, _stream(k)))
+    _launch(load().basa_cache_append, k, C.byref(kd), C.byref(vd), at, *cache._keys)
 
 
 def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=None):
@@ -519,17 +523,20 @@ def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=Non
     if k.shape[0] != tokens or v.shape != k.shape:
         raise ValueError("out: two tensors of `tokens` rows")
     if tokens:
-        with _on_device(cache.device):
-            _check(load().basa_cache_gather(*cache._keys, tab, width, stride, cu, n, C.byref(kd), C.byref(vd), _stream(k)))
+        _launch(load().basa_cache_gather, k, *cache._keys, tab, width, stride, cu, n, C.byref(kd), C.byref(vd))
     return k, v
 
 
 def _token_desc(q: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
     """Descriptor of one token per sequence, [batch, heads, d]."""
-    if q.dim() != 3 or q.dtype != cache.dtype or q.device != cache.device or q.stride(2) != 1:
+    shape = q.shape
+    if len(shape) != 3 or q.dtype != cache.dtype or q.device != cache.device or q.stride(2) != 1:
         raise ValueError(f"{name} must be a {cache.dtype} tensor [batch, heads, d] on {cache.device} with a contiguous d axis")
-    b, h, d = q.shape
-    return BasaTensor(q.data_ptr(), _DTYPES[q.dtype], b, h, 1, d, q.stride(0) if b > 1 else 0, q.stride(1) if h > 1 else 0, d)
+    (b, h, d), (sb, sh, _) = shape, q.stride()
+    return BasaTensor(q.data_ptr(), cache._kd.dtype, b, h, 1, d, sb if b > 1 else 0, sh if h > 1 else 0, d)
+
+
+_TwoStrides = C.c_int64 * 2
 
 
 def decode_workspace_size(q, cache: PagedCache, table) -> int:
@@ -553,10 +560,9 @@ def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, 
         qr = C.byref(qd)
         if ws is None:
             ws = _ws(lib.basa_decode_workspace_size(qr, *cache._keys, width), dev)
-        ostr = (C.c_int64 * 2)(out.stride(0) if b > 1 else 0, out.stride(1) if hq > 1 else d)
-        with _on_device(dev):
-            _check(lib.basa_decode_attn(qr, *cache._keys, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel(),
-                                        _stream(q)))
+        sb, sh, _ = out.stride()
+        ostr = _TwoStrides(sb if b > 1 else 0, sh if hq > 1 else d)
+        _launch(lib.basa_decode_attn, q, qr, *cache._keys, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel())
     return (out, lse) if want_lse else out
 
 

@@ -407,7 +407,13 @@ basa_status check_decode(const basa_tensor* q, const basa_tensor* k, const basa_
   }
   if ((int64_t)q->batch * q->heads > kMaxPagedTokens) { set_error("q: batch*heads exceeds %d", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
   static const int32_t some = 0;
-  return check_table(&some, q->batch, width, width, k->L);
+  if ((s = check_table(&some, q->batch, width, width, k->L)) != BASA_OK) return s;
+  if (!decode_takes(q->batch, q->heads, k->heads, q->dtype == BASA_BF16, width * k->L)) {
+    set_error("%d sequences of %d KV heads with room for %lld tokens each: more steps than a call takes", q->batch, k->heads,
+              (long long)width * k->L);
+    return BASA_ERR_UNSUPPORTED;
+  }
+  return BASA_OK;
 }
 
 }  // namespace
@@ -793,7 +799,7 @@ basa_status basa_cache_gather(const basa_tensor* k_pages, const basa_tensor* v_p
 
 size_t basa_decode_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t width) {
   if (check_decode(q, k_pages, v_pages, width) != BASA_OK) return 0;
-  return decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, (int64_t)width * k_pages->L);
+  return decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
 }
 
 basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table,
@@ -814,7 +820,7 @@ basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, c
       return BASA_ERR_INVALID_ARG;
     }
   }
-  const size_t need = decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, (int64_t)width * k_pages->L);
+  const size_t need = decode_workspace_bytes(q->batch, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
   if (!ws || ws_bytes < need) {
     set_error("decode workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
     return BASA_ERR_WORKSPACE;

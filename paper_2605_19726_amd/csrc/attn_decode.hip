@@ -39,21 +39,29 @@ struct DecodeArgs {
   const int32_t *table, *lens;
   int64_t table_stride;
   int batch, heads_kv, group, units, pages; // units: runs of 16 kNT query heads that share a KV head
-  int64_t row_tokens;                       // tokens a table row has room for
+  int row_tokens;                           // tokens a table row has room for
   FastDiv page;
   char* out;
   int64_t out_b, out_h;                     // in bytes
   float* lse;                               // [batch][heads_q] or null
-  int groups;                               // workgroups
-  int64_t* first_place;                     // workspace: [batch + 1], the last one the length of a run
+  int* first_place;                         // workspace: [batch + 1], the last one the length of a run
   int part_heads;                           // query heads of a partial result
   float* part_o;                            // [2 groups][part_heads][d], not normalised
   float2* part_ml;                          // [2 groups][part_heads] maximum, sum
   float scale, scale_log2e;
 };
 
-__device__ __forceinline__ int64_t cached_tokens(const DecodeArgs& a, int b) {
-  return min(max((int64_t)a.lens[b], (int64_t)0), a.row_tokens);
+__device__ __forceinline__ int cached_tokens(const DecodeArgs& a, int b) { return min(max(a.lens[b], 0), a.row_tokens); }
+// Sum over this lane and the ones before it.
+__device__ __forceinline__ int wave_scan(int x) {
+  constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+  x += __builtin_amdgcn_update_dpp(0, x, kRowShr1, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kRowShr2, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kRowShr4, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kRowShr8, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kRowBcast15, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, kRowBcast31, 0xc, 0xf, false);
+  return x;
 }
 __device__ __forceinline__ float column_max(float v) {      // over the four lane groups
   uint32_t x, y;
@@ -92,74 +100,73 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
   }
 }
 
-template <bool kBf16, int kD, int kNT>
-__global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
-  constexpr int kHeads = 16 * kNT, kElem = kBf16 ? 2 : 4;
+// kSplit: the cut by runs.  Otherwise a workgroup per (sequence, run of query heads).
+template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit>
+__global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
+  constexpr int kHeads = 16 * kNT, kElem = kBf16 ? 2 : 4, kThreads = 64 * kWaves;
   constexpr int kKSteps = kD * kElem / 64;               // 16-byte chunks of a K row per lane
   constexpr int kBlocks = kD / 16;                       // output blocks of 16 dimensions
   constexpr int kVLoads = kBf16 ? 1 : kD / 64;           // loads of a V row per lane: kD / 16 numbers (bf16), 4 at a time (f32)
-  __shared__ int64_t row_at[kDecodeWaves][2][kDecodeTile];
-  __shared__ float part[kDecodeWaves][kHeads][kD + 4];
-  __shared__ float2 part_ml[kDecodeWaves][kHeads];
-  __shared__ int64_t wave_sum[4], found_first;
-  __shared__ int found;
+  constexpr int kPitch = kD + 4;
+  extern __shared__ __attribute__((aligned(16))) float part[];        // [kWaves][part_heads][kPitch], then their maxima and sums
+  __shared__ int64_t row_at[kWaves][2][kDecodeTile];         // K, V
+  float2* const part_ml = reinterpret_cast<float2*>(part + kWaves * a.part_heads * kPitch);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
+  const int per_seq = a.heads_kv * a.units;
 
-  // the run of this workgroup and the sequence that its first place is of
-  const int64_t per_seq = (int64_t)a.heads_kv * a.units;
-  const int each = (a.batch + 255) / 256, i0 = min(tid * each, a.batch), i1 = min(i0 + each, a.batch);
-  int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) mine += decode_places(cached_tokens(a, i)) * per_seq;
-  int64_t x = mine;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t y = __shfl_up(x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 63) wave_sum[wave] = x;
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __syncthreads();
-  int64_t before = x - mine, total = 0;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    if (w < wave) before += wave_sum[w];
-    total += wave_sum[w];
-  }
-  const int64_t run = decode_run(total), begin = blockIdx.x * run, end = min(begin + run, total);
-  if (begin >= total) return;
-  if (before <= begin && begin < before + mine) {
-    int i = i0;
-    int64_t at = before;
-    for (;; ++i) {
-      const int64_t n = decode_places(cached_tokens(a, i)) * per_seq;
-      if (begin < at + n) break;
-      at += n;
+  // the run of this workgroup and the sequence that its first place is of: every wave finds them for itself, a run of sequences to a lane
+  int b = 0, first = 0, run = 0, begin = 0, end = 1;
+  if constexpr (kSplit) {
+    const int each = (a.batch + 63) / 64, i0 = min(lane * each, a.batch), i1 = min(i0 + each, a.batch);
+    int mine = 0;
+    for (int i = i0; i < i1; ++i) mine += decode_places(cached_tokens(a, i));
+    const int upto = wave_scan(mine);
+    const int total = __builtin_amdgcn_readlane(upto, 63) * per_seq;
+    run = decode_run(total);
+    begin = blockIdx.x * run;
+    end = min(begin + run, total);
+    if (begin >= total) return;
+    const int seq_place = begin / per_seq;      // as if all heads lay side by side: places [seq_place, ..) of one head
+    const int at = __builtin_ctzll(__ballot(upto > seq_place));
+    first = __builtin_amdgcn_readlane(upto - mine, at);
+    b = at * each;
+    for (;; ++b) {
+      const int n = decode_places(cached_tokens(a, b));
+      if (seq_place < first + n) break;
+      first += n;
     }
-    found = i;
-    found_first = at;
+    first *= per_seq;
+    if (blockIdx.x == 0 && tid == 0) a.first_place[a.batch] = run;
+  } else {
+    b = blockIdx.x / per_seq;
   }
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-  __syncthreads();
-  int b = __builtin_amdgcn_readfirstlane(found);
-  int64_t first = found_first;
-  if (blockIdx.x == 0 && tid == 0) a.first_place[a.batch] = run;
 
-  for (int64_t pos = begin; pos < end;) {
-    const int len = (int)cached_tokens(a, b), steps = (int)decode_steps(len);
-    const int unit = (int)((pos - first) / (steps + kDecodeLead));
-    const int64_t seq_first = first, head_first = first + (int64_t)unit * (steps + kDecodeLead);
-    const DecodePiece piece = decode_piece(head_first, steps, blockIdx.x, run);
-    const int seq = b;
-    pos = head_first + steps + kDecodeLead;
-    if (unit + 1 == per_seq) {
-      ++b;
-      first = pos;
+  for (int pos = begin; pos < end;) {
+    const int len = cached_tokens(a, b), seq = b;
+    int unit, t0 = 0, t1 = (len + kDecodeTile - 1) / kDecodeTile, place = 0;      // tiles
+    bool whole = true;
+    if constexpr (kSplit) {
+      const int steps = decode_steps(len), seq_first = first;
+      unit = (pos - first) / (steps + kDecodeLead);
+      const int head_first = first + unit * (steps + kDecodeLead);
+      const DecodePiece piece = decode_piece(head_first, steps, blockIdx.x, run);
+      pos = head_first + steps + kDecodeLead;
+      if (unit + 1 == per_seq) {
+        ++b;
+        first = pos;
+      }
+      if (piece.t1 <= piece.t0) continue;      // the run ends before its first step
+      t0 = piece.t0 * kDecodeWaves;
+      t1 = min(t1, piece.t1 * kDecodeWaves);
+      whole = piece.t0 == 0 && piece.t1 == steps;
+      place = decode_part(piece, blockIdx.x);
+      if (unit == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
+    } else {
+      unit = blockIdx.x - b * per_seq;
+      pos = end;
     }
-    if (piece.t1 <= piece.t0) continue;      // the run ends before its first step
-    const int t0 = (int)piece.t0 * kDecodeWaves, t1 = min((int)piece.t1 * kDecodeWaves, (len + kDecodeTile - 1) / kDecodeTile);   // tiles
     const int kvh = unit / a.units, h0 = kvh * a.group + (unit - kvh * a.units) * kHeads;
     const int heads = min(kHeads, (kvh + 1) * a.group - h0);
-    if (unit == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
 
     // queries: lane (g, n) holds chunk 4 c + g of head n
     uintx4 qf[kNT][kKSteps];
@@ -183,22 +190,23 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
     const char* k_head = a.k + kvh * a.k_h;
     const char* v_head = a.v + kvh * a.v_h;
     const int64_t page_stride = lane < 32 ? a.k_b : a.v_b, row_stride = lane < 32 ? a.k_l : a.v_l;
-    int page_id = -1, page_off = 0;
+    int page_id, page_off;
     auto look_up = [&](int t) {               // the page of the lane's token of tile t; both halves of the wave: the same tokens
-      const int64_t tok = (int64_t)t * kDecodeTile + (lane & 31);
+      const int tok = t * kDecodeTile + (lane & 31);
       page_id = -1;
+      page_off = 0;
       if (t < t1 && tok < len) {
-        const int p = (int)a.page.div((uint32_t)tok);
-        page_off = (int)tok - p * (int)a.page.d;
+        const int p = (int)a.page.div(tok);
+        page_off = tok - p * (int)a.page.d;
         page_id = table[p];
       }
     };
     look_up(t0 + wave);
-    for (int t = t0 + wave; t < t1; t += kDecodeWaves) {
+    for (int t = t0 + wave; t < t1; t += kWaves) {
       const bool valid = (unsigned)page_id < (unsigned)a.pages;
       const uint32_t live = (uint32_t)__ballot(valid);
       row_at[wave][lane >> 5][lane & 31] = valid ? page_id * page_stride + page_off * row_stride : 0;
-      look_up(t + kDecodeWaves);
+      look_up(t + kWaves);
       uintx4 kf[2][kKSteps];
 #pragma unroll
       for (int s = 0; s < 2; ++s)
@@ -326,77 +334,82 @@ __global__ __launch_bounds__(256, 2) void decode_kernel(DecodeArgs a) {
       }
     }
 
-    // the four waves together.  Block e, register i of lane (g, n): head n; dimension kBlocks (4 g + i) + e (bf16), 64 (e / 4) + 4 (4 g + i) +
+    // the waves together.  Block e, register i of lane (g, n): head n; dimension kBlocks (4 g + i) + e (bf16), 64 (e / 4) + 4 (4 g + i) +
     // e % 4 (f32)
 #pragma unroll
     for (int nt = 0; nt < kNT; ++nt) {
       const int h = nt * 16 + r;
       const float sum = column_sum(l[nt]);
       if (h < heads) {
-        if (g == 0) part_ml[wave][h] = make_float2(m[nt], sum);
+        const int row = wave * a.part_heads + h;
+        if (g == 0) part_ml[row] = make_float2(m[nt], sum);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
           for (int e = 0; e < kBlocks; e += 4) {
             const int dim = kBf16 ? kBlocks * (4 * g + i) + e : 16 * e + 4 * (4 * g + i);
-            *reinterpret_cast<floatx4*>(&part[wave][h][dim]) = floatx4{acc[nt][e][i], acc[nt][e + 1][i], acc[nt][e + 2][i], acc[nt][e + 3][i]};
+            *reinterpret_cast<floatx4*>(part + row * kPitch + dim) = floatx4{acc[nt][e][i], acc[nt][e + 1][i], acc[nt][e + 2][i], acc[nt][e + 3][i]};
           }
       }
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
-    const bool whole = piece.t0 == 0 && piece.t1 == steps;
-    const int64_t place = decode_part(piece, blockIdx.x) * a.part_heads;
-    for (int i = tid; i < heads * (kD / 4); i += 256) {
+    for (int i = tid; i < heads * (kD / 4); i += kThreads) {
       const int h = i / (kD / 4), c = i % (kD / 4);
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, part_ml[w][h].x);
+      for (int w = 0; w < kWaves; ++w) top = fmaxf(top, part_ml[w * a.part_heads + h].x);
       floatx4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int w = 0; w < kDecodeWaves; ++w) {
-        const float2 ml = part_ml[w][h];
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 ml = part_ml[w * a.part_heads + h];
         const float f = weight_of(ml.x, top, a.scale_log2e);
         sum = fmaf(ml.y, f, sum);
-        o += *reinterpret_cast<const floatx4*>(&part[w][h][4 * c]) * f;
+        o += *reinterpret_cast<const floatx4*>(part + (w * a.part_heads + h) * kPitch + 4 * c) * f;
       }
       if (whole) {
         store4<kBf16>(a.out + seq * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
         if (a.lse && c == 0) a.lse[(int64_t)seq * a.heads_kv * a.group + h0 + h] = lse_of(top, sum, a.scale);
       } else {
-        *reinterpret_cast<floatx4*>(a.part_o + (place + h) * kD + 4 * c) = o;
-        if (c == 0) a.part_ml[place + h] = make_float2(top, sum);
+        const int64_t at = (int64_t)place * a.part_heads + h;
+        *reinterpret_cast<floatx4*>(a.part_o + at * kD + 4 * c) = o;
+        if (c == 0) a.part_ml[at] = make_float2(top, sum);
       }
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __syncthreads();
+    if constexpr (kSplit) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      __syncthreads();
+    }
   }
 }
 
 // The pieces of a (sequence, query head) that more than one workgroup had a part in, added up: a workgroup per sequence and head, 4 numbers to
 // a lane, every 256 / (d / 4)-th part to a lane group, four of them requested at once.
-constexpr int kPartsAtOnce = 4;
-template <bool kBf16, int kD>
+// With many rows, whose sequences are cut into few parts if at all, a wave takes one and a workgroup four.
+constexpr int kPartsAtOnce = 4, kCUs = 256;
+template <bool kBf16, int kD, int kAtOnce>
 __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int heads_per_unit) {
-  constexpr int kLanes = kD / 4, kRows = 256 / kLanes, kElem = kBf16 ? 2 : 4;
-  __shared__ floatx4 row_o[kRows][kLanes];
-  __shared__ float2 row_ml[kRows];
-  const int heads_q = a.heads_kv * a.group, b = blockIdx.x / heads_q, head = blockIdx.x - b * heads_q;
+  constexpr int kLanes = kD / 4, kThreads = 256 / kAtOnce, kRows = kThreads / kLanes, kElem = kBf16 ? 2 : 4;
+  __shared__ floatx4 row_o[kAtOnce][kRows][kLanes];
+  __shared__ float2 row_ml[kAtOnce][kRows];
+  const int tid = threadIdx.x % kThreads, mine = threadIdx.x / kThreads;
+  const int heads_q = a.heads_kv * a.group, id = min((int)blockIdx.x * kAtOnce + mine, a.batch * heads_q - 1), b = id / heads_q, head = id - b * heads_q;
   const int kvh = head / a.group, sub = (head - kvh * a.group) / heads_per_unit, h = head - kvh * a.group - sub * heads_per_unit;
-  const int64_t run = a.first_place[a.batch], steps = decode_steps(cached_tokens(a, b));
-  const int64_t first = a.first_place[b] + (int64_t)(kvh * a.units + sub) * (steps + kDecodeLead);
-  const int g0 = (int)decode_first_group(first, run), g1 = (int)decode_last_group(first, steps, run);
-  if (g0 == g1) return;
-  const int c = threadIdx.x % kLanes, row = threadIdx.x / kLanes;
+  const int run = a.first_place[a.batch], steps = decode_steps(cached_tokens(a, b));
+  const int first = a.first_place[b] + (kvh * a.units + sub) * (steps + kDecodeLead);
+  const int g0 = decode_first_group(first, run), g1 = decode_last_group(first, steps, run);
+  const bool split = g0 != g1 && (kAtOnce == 1 || id == (int)blockIdx.x * kAtOnce + mine);
+  if (kAtOnce == 1 && !split) return;
+  const int c = tid % kLanes, row = tid / kLanes;
   float m = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int w0 = g0 + row; w0 <= g1; w0 += kRows * kPartsAtOnce) {
+  for (int w0 = g0 + row; split && w0 <= g1; w0 += kRows * kPartsAtOnce) {
     float2 ml[kPartsAtOnce];
     floatx4 p[kPartsAtOnce];
 #pragma unroll
     for (int j = 0; j < kPartsAtOnce; ++j) {
       const int w = min(w0 + j * kRows, g1);
-      const int64_t place = decode_part(decode_piece(first, steps, w, run), w) * a.part_heads + h;
+      const int64_t place = (int64_t)decode_part(decode_piece(first, steps, w, run), w) * a.part_heads + h;
       ml[j] = a.part_ml[place];
       p[j] = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
     }
@@ -415,60 +428,82 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
       o += p[j] * f;
     }
   }
-  row_o[row][c] = o;
-  if (c == 0) row_ml[row] = make_float2(m, l);
+  row_o[mine][row][c] = o;
+  if (c == 0) row_ml[mine][row] = make_float2(m, l);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
-  if (row > 0) return;
+  if (row > 0 || !split) return;
   float top = -INFINITY, sum = 0.f;
 #pragma unroll
-  for (int i = 0; i < kRows; ++i) top = fmaxf(top, row_ml[i].x);
+  for (int i = 0; i < kRows; ++i) top = fmaxf(top, row_ml[mine][i].x);
   o = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < kRows; ++i) {
-    const float f = weight_of(row_ml[i].x, top, a.scale_log2e);
-    sum = fmaf(row_ml[i].y, f, sum);
-    o += row_o[i][c] * f;
+    const float f = weight_of(row_ml[mine][i].x, top, a.scale_log2e);
+    sum = fmaf(row_ml[mine][i].y, f, sum);
+    o += row_o[mine][i][c] * f;
   }
   store4<kBf16>(a.out + b * a.out_b + head * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
-  if (a.lse && c == 0) a.lse[blockIdx.x] = lse_of(top, sum, a.scale);
+  if (a.lse && c == 0) a.lse[id] = lse_of(top, sum, a.scale);
 }
 
 // Query heads that share the loads of their KV head: up to 32 (bf16), 16 (f32, whose rows take twice the registers).
 int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
-int most_groups(int batch, int heads_kv, int group, bool bf16, int64_t row_tokens) {
-  return decode_groups((int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens));
+// One workgroup of 8 waves for all of a (sequence, run of query heads): no cut, no join, one launch.  A compute unit takes in some 64 GB/s, 2.2 us
+// for 256 tokens of bf16, d = 128, whatever its waves do; so that is for calls that are short, or have a workgroup for every compute unit and are
+// not long.  One launch -> two (32 heads on 8, d = 128): one sequence of 256 tokens 6.1 -> 5.7 + 3.4 us on the device, of 700 10.6 -> 5.8 + 3.4, of
+// 1024 12.8 -> 5.7 + 3.4; from the host 10.3 -> 12.4 for all of them; 64 of 200 to 1000 31.7 -> 28.5 + 4.5, 16 of 1000 18.1 -> 16.0 + 4.1.
+bool is_solo(int64_t units, int row_tokens) { return row_tokens <= 768 || (row_tokens <= 1024 && units >= kCUs / 2); }
+int64_t most_places(int batch, int heads_kv, int group, bool bf16, int row_tokens) {
+  return (int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens);
 }
 struct DecodeWs { size_t first_place, part_o, part_ml, total; };
 DecodeWs carve(int batch, int groups, int part_heads, int d) {
   DecodeWs w;
   size_t o = 0;
-  w.first_place = o; o += align_up((size_t)(batch + 1) * 8, 256);
+  w.first_place = o; o += align_up((size_t)(batch + 1) * 4, 256);
   w.part_o = o; o += align_up((size_t)2 * groups * part_heads * d * 4, 256);
   w.part_ml = o; o += align_up((size_t)2 * groups * part_heads * 8, 256);
   w.total = o;
   return w;
 }
 
-template <bool kBf16, int kD, int kNT>
-basa_status launch(const DecodeArgs& a, hipStream_t st) {
-  {
-    ProfScope prof(K_DECODE, st);
-    decode_kernel<kBf16, kD, kNT><<<a.groups, 256, 0, st>>>(a);
-    BASA_HIP_CHECK_LAUNCH("decode_kernel");
+template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit>
+basa_status launch_kernel(const DecodeArgs& a, int groups, hipStream_t st) {
+  const auto kernel = decode_kernel<kBf16, kD, kNT, kWaves, kSplit>;
+  const int lds = kWaves * a.part_heads * ((kD + 4) * 4 + 8);
+  if (lds > 60 * 1024) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(dynamic LDS)");
   }
-  if (a.row_tokens <= kDecodeStep) return BASA_OK;        // nothing to split
+  ProfScope prof(K_DECODE, st);
+  kernel<<<groups, 64 * kWaves, lds, st>>>(a);
+  BASA_HIP_CHECK_LAUNCH("decode_kernel");
+  return BASA_OK;
+}
+template <bool kBf16, int kD, int kNT>
+basa_status launch(const DecodeArgs& a, int groups, hipStream_t st) {
+  const int64_t units = (int64_t)a.batch * a.heads_kv * a.units;
+  if (is_solo(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 8, false>(a, (int)units, st);
+  const basa_status s = launch_kernel<kBf16, kD, kNT, kDecodeWaves, true>(a, groups, st);
+  if (s != BASA_OK) return s;
   ProfScope prof(K_DECODE_JOIN, st);
-  decode_join_kernel<kBf16, kD><<<a.batch * a.heads_kv * a.group, 256, 0, st>>>(a, 16 * kNT);
+  const int rows = a.batch * a.heads_kv * a.group;
+  if (rows < 4 * kCUs) decode_join_kernel<kBf16, kD, 1><<<rows, 256, 0, st>>>(a, 16 * kNT);
+  else decode_join_kernel<kBf16, kD, 4><<<ceil_div(rows, 4), 256, 0, st>>>(a, 16 * kNT);
   BASA_HIP_CHECK_LAUNCH("decode_join_kernel");
   return BASA_OK;
 }
 
 }  // namespace
 
-size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int64_t row_tokens) {
+bool decode_takes(int batch, int heads_q, int heads_kv, bool bf16, int row_tokens) {
+  return most_places(batch, heads_kv, heads_q / heads_kv, bf16, row_tokens) < INT_MAX - kDecodeMost;
+}
+size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int row_tokens) {
   const int group = heads_q / heads_kv;
-  return carve(batch, most_groups(batch, heads_kv, group, bf16, row_tokens), std::min(group, heads_per_unit(group, bf16)), d).total;
+  if (is_solo((int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)), row_tokens)) return 256;
+  return carve(batch, decode_groups(most_places(batch, heads_kv, group, bf16, row_tokens)), std::min(group, heads_per_unit(group, bf16)), d).total;
 }
 
 basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
@@ -483,23 +518,23 @@ basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, c
   a.v_b = v_pages.stride_b * e; a.v_h = v_pages.stride_h * e; a.v_l = v_pages.stride_l * e;
   a.table = table; a.table_stride = table_stride; a.lens = lens;
   a.batch = q.batch; a.heads_kv = k_pages.heads; a.group = q.heads / k_pages.heads; a.pages = k_pages.batch;
-  a.row_tokens = (int64_t)width * k_pages.L;
+  a.row_tokens = width * k_pages.L;
   a.page = fast_div((uint32_t)k_pages.L);
   const int hpu = heads_per_unit(a.group, bf16);
   a.units = ceil_div(a.group, hpu);
   a.out = static_cast<char*>(out); a.out_b = out_sb * e; a.out_h = out_sh * e; a.lse = lse;
-  a.groups = most_groups(a.batch, a.heads_kv, a.group, bf16, a.row_tokens);
+  const int groups = decode_groups(most_places(a.batch, a.heads_kv, a.group, bf16, a.row_tokens));
   a.part_heads = std::min(a.group, hpu);
-  const DecodeWs w = carve(a.batch, a.groups, a.part_heads, q.d);
+  const DecodeWs w = carve(a.batch, groups, a.part_heads, q.d);
   char* base = static_cast<char*>(ws);
-  a.first_place = reinterpret_cast<int64_t*>(base + w.first_place);
+  a.first_place = reinterpret_cast<int*>(base + w.first_place);
   a.part_o = reinterpret_cast<float*>(base + w.part_o);
   a.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   a.scale = 1.0f / sqrtf((float)q.d);
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)q.d);
-  if (!bf16) return q.d == 128 ? launch<false, 128, 1>(a, st) : launch<false, 64, 1>(a, st);
-  if (hpu == 16) return q.d == 128 ? launch<true, 128, 1>(a, st) : launch<true, 64, 1>(a, st);
-  return q.d == 128 ? launch<true, 128, 2>(a, st) : launch<true, 64, 2>(a, st);
+  if (!bf16) return q.d == 128 ? launch<false, 128, 1>(a, groups, st) : launch<false, 64, 1>(a, groups, st);
+  if (hpu == 16) return q.d == 128 ? launch<true, 128, 1>(a, groups, st) : launch<true, 64, 1>(a, groups, st);
+  return q.d == 128 ? launch<true, 128, 2>(a, groups, st) : launch<true, 64, 2>(a, groups, st);
 }
 
 }  // namespace basa

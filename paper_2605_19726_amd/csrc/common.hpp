@@ -185,7 +185,8 @@ basa_status launch_cache_append(const TensorView& k, const TensorView& v, const 
                                 const TensorView& v_pages, hipStream_t st);
 basa_status launch_cache_gather(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                                 int64_t table_stride, const int32_t* cu, int n, const TensorView& k, const TensorView& v, hipStream_t st);
-size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int64_t row_tokens);
+bool decode_takes(int batch, int heads_q, int heads_kv, bool bf16, int row_tokens);
+size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
 basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                                int64_t table_stride, const int32_t* lens, void* out, int64_t out_sb, int64_t out_sh, float* lse, void* ws,
                                hipStream_t st);

@@ -34,32 +34,34 @@ inline FastDiv fast_div(uint32_t d) {
 // cut into runs of equal length; workgroup w takes what lies in [w run, (w + 1) run).
 constexpr int kDecodeTile = 32, kDecodeWaves = 4, kDecodeStep = kDecodeTile * kDecodeWaves;
 constexpr int kDecodeLead = 1;
-BASA_HD int64_t decode_steps(int64_t len) { return len <= kDecodeStep ? 1 : (len + kDecodeStep - 1) / kDecodeStep; }
-BASA_HD int64_t decode_places(int64_t len) { return decode_steps(len) + kDecodeLead; }
-constexpr int kDecodeFew = 512, kDecodeMost = 3072, kDecodeLongRun = 32;
-BASA_HD int64_t decode_run(int64_t total) {
-  const int64_t few = (total + kDecodeFew - 1) / kDecodeFew, many = (total + kDecodeMost - 1) / kDecodeMost;
-  return few <= kDecodeLongRun ? few : many > kDecodeLongRun ? many : kDecodeLongRun;
+BASA_HD int decode_steps(int len) { return len <= kDecodeStep ? 1 : (len + kDecodeStep - 1) / kDecodeStep; }
+BASA_HD int decode_places(int len) { return decode_steps(len) + kDecodeLead; }
+// The length of a run: two workgroups fit a compute unit, so short rows are cut into as many runs as there is room for at once.  Where
+// those would be longer than 24 steps there are more, down to 8 steps, so that a workgroup that is done early is followed by another; 3072
+// at most, which is as far as that helps.  Main kernel + join, one round -> runs of 8 and more: 1024 (sequence, head) of 2000 tokens, d = 128:
+// 205 + 4 -> 167 + 4 us; 2048 of 100 to 4000: 218 + 10.5 -> 185 + 11; one sequence of 128K tokens, 8 heads (17 steps): 86 + 5.8, in runs
+// of 8 89 + 9.3.
+constexpr int kDecodeOneRound = 512, kDecodeMost = 3072, kDecodeLongRun = 24, kDecodeShortRun = 8;
+BASA_HD int decode_run(int total) {          // total < 2^31 - kDecodeMost
+  const int one = (total + kDecodeOneRound - 1) / kDecodeOneRound, many = (total + kDecodeMost - 1) / kDecodeMost;
+  return one <= kDecodeLongRun ? one : many > kDecodeShortRun ? many : kDecodeShortRun;
 }
 // What lies in a run of a (sequence, head) whose first place is `first`: steps [t0, t1), none if t1 <= t0.
-struct DecodePiece { int64_t t0, t1; };
-BASA_HD DecodePiece decode_piece(int64_t first, int64_t steps, int64_t group, int64_t run) {
-  const int64_t begin = group * run - first - kDecodeLead, end = begin + run;
+struct DecodePiece { int t0, t1; };
+BASA_HD DecodePiece decode_piece(int first, int steps, int group, int run) {
+  const int64_t begin = (int64_t)group * run - first - kDecodeLead, end = begin + run;
   DecodePiece p;
-  p.t0 = begin > 0 ? begin : 0;
-  p.t1 = end < steps ? end : steps;
+  p.t0 = begin > 0 ? (int)(begin < steps ? begin : steps) : 0;
+  p.t1 = end < steps ? (end > 0 ? (int)end : 0) : steps;
   return p;
 }
 // A run holds at most two pieces that are not whole: the end or middle of one that began before it, which has place 0 of the run's two
 // partial results, and the beginning of one that goes on behind it, place 1.
-BASA_HD int64_t decode_part(DecodePiece p, int64_t group) { return 2 * group + (p.t0 == 0 ? 1 : 0); }
+BASA_HD int decode_part(DecodePiece p, int group) { return 2 * group + (p.t0 == 0 ? 1 : 0); }
 // The groups that have steps of it: first and last.
-BASA_HD int64_t decode_first_group(int64_t first, int64_t run) { return (first + kDecodeLead) / run; }
-BASA_HD int64_t decode_last_group(int64_t first, int64_t steps, int64_t run) { return (first + kDecodeLead + steps - 1) / run; }
-// Workgroups of a call of up to `total` places, whatever the lengths turn out to be.
-inline int decode_groups(int64_t most) {
-  const int64_t n = most < kDecodeMost ? most : kDecodeMost;
-  return (int)n;
-}
+BASA_HD int decode_first_group(int first, int run) { return (first + kDecodeLead) / run; }
+BASA_HD int decode_last_group(int first, int steps, int run) { return (first + kDecodeLead + steps - 1) / run; }
+// Workgroups of a call of up to `most` places, whatever the lengths turn out to be.
+inline int decode_groups(int64_t most) { return (int)(most < kDecodeMost ? most : kDecodeMost); }
 
 }  // namespace basa
