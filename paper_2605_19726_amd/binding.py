@@ -435,13 +435,19 @@ class PagedCache:
 
 class PageTables:
     """Outputs of basa_page_tables (device tensors) for n_seq sequences and up to `tokens` new tokens."""
-    __slots__ = ("slots", "lens", "cu", "pages")
+    __slots__ = ("_n", "_tokens", "_device", "_outs", "_ptrs")
 
     def __init__(self, n_seq: int, tokens: int, device):
-        self.slots = torch.empty(tokens, dtype=torch.int64, device=device)
-        self.lens = torch.empty(n_seq, dtype=torch.int32, device=device)
-        self.cu = torch.empty(n_seq + 1, dtype=torch.int32, device=device)
-        self.pages = torch.empty(2, dtype=torch.int32, device=device)
+        device = torch.device(device)
+        slots = torch.empty(int(tokens), dtype=torch.int64, device=device)
+        ints = [torch.empty(n, dtype=torch.int32, device=device) for n in (n_seq, n_seq + 1, 2)]
+        self._n, self._tokens, self._device, self._outs = n_seq, int(tokens), slots.device, (slots, *ints)
+        self._ptrs = tuple(t.data_ptr() for t in self._outs)
+
+    slots = property(lambda self: self._outs[0], doc="[tokens] int64: slot of every new token, -1 for none")
+    lens = property(lambda self: self._outs[1], doc="[n_seq] int32: tokens that a sequence holds after the step")
+    cu = property(lambda self: self._outs[2], doc="[n_seq + 1] int32: first new token of every sequence")
+    pages = property(lambda self: self._outs[3], doc="[2] int32: free pages given out, and asked for")
 
 
 def _int_array(t: torch.Tensor, name: str, device, shape, dtype=torch.int32):
@@ -488,12 +494,12 @@ def basa_page_tables(have, add, table, free_pages, page: int, tokens: int, out: 
     lib, dev, n = load(), table.device, have.shape[0]
     tab, width, stride = _block_table(table, n, dev)
     if out is None:
-        out = PageTables(n, int(tokens), dev)
-    one = (n,)
-    args = (_int_array(have, "have", dev, one), _int_array(add, "add", dev, one), n, int(page), tab, width, stride,
-            _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0],
-            _int_array(out.slots, "slots", dev, (int(tokens),), torch.int64), int(tokens), _int_array(out.lens, "lens", dev, one),
-            _int_array(out.cu, "cu", dev, (n + 1,)), _int_array(out.pages, "pages", dev, (2,)))
+        out = PageTables(n, tokens, dev)
+    elif out._n != n or out._tokens != tokens or out._device != dev:
+        raise ValueError(f"out: a PageTables({n}, {tokens}, {dev})")
+    slots, lens, cu, pages = out._ptrs
+    args = (_int_array(have, "have", dev, (n,)), _int_array(add, "add", dev, (n,)), n, int(page), tab, width, stride,
+            _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0], slots, int(tokens), lens, cu, pages)
     _launch(lib.basa_page_tables, table, *args)
     return out
 

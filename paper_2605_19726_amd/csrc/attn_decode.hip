@@ -454,6 +454,11 @@ int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; 
 // not long.  One launch -> two (32 heads on 8, d = 128): one sequence of 256 tokens 6.1 -> 5.7 + 3.4 us on the device, of 700 10.6 -> 5.8 + 3.4, of
 // 1024 12.8 -> 5.7 + 3.4; from the host 10.3 -> 12.4 for all of them; 64 of 200 to 1000 31.7 -> 28.5 + 4.5, 16 of 1000 18.1 -> 16.0 + 4.1.
 bool is_solo(int64_t units, int row_tokens) { return row_tokens <= 768 || (row_tokens <= 1024 && units >= kCUs / 2); }
+// Many short rows: workgroups of 2 waves, of which each compute unit holds more, so that the end of one overlaps others; a line between rows
+// that are long beside their number and the reverse.  8 waves -> 2: 1600 rows of 1 to 60 tokens 17.9 -> 8.7 us, 1600 of 60 to 120 23 -> 16, 1024 of
+// 20 to 500 24.8 -> 22.5, 8000 of 100 to 250 145 -> 114, 8000 of 100 to 1000 299 -> 277; level: 2048 of 100 to 1000 (80 / 81); kept at 8: 64 rows
+// of 100 to 250 6.7 / 9.4, 1024 of 20 to 1000 (d = 64) 20 / 24.
+bool has_small_workgroups(int64_t units, int row_tokens) { return units >= 2 * row_tokens; }
 int64_t most_places(int batch, int heads_kv, int group, bool bf16, int row_tokens) {
   return (int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens);
 }
@@ -484,6 +489,7 @@ basa_status launch_kernel(const DecodeArgs& a, int groups, hipStream_t st) {
 template <bool kBf16, int kD, int kNT>
 basa_status launch(const DecodeArgs& a, int groups, hipStream_t st) {
   const int64_t units = (int64_t)a.batch * a.heads_kv * a.units;
+  if (is_solo(units, a.row_tokens) && has_small_workgroups(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 2, false>(a, (int)units, st);
   if (is_solo(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 8, false>(a, (int)units, st);
   const basa_status s = launch_kernel<kBf16, kD, kNT, kDecodeWaves, true>(a, groups, st);
   if (s != BASA_OK) return s;
