@@ -84,10 +84,13 @@ __device__ __forceinline__ float weight_of(float s, float m, float scale_log2e) 
 __device__ __forceinline__ float lse_of(float m, float l, float scale) {
   return l == 0.f ? -INFINITY : fmaf(m, scale, __logf(l));
 }
-// The cache is read once: its lines are the first to leave the L2.  (Pays only where an instruction takes whole lines of 128 bytes; with half
-// lines, whose other half is asked for by the next instruction, they leave before that.)
-template <class T>
-__device__ __forceinline__ T load_once(const char* at) { return __builtin_nontemporal_load(reinterpret_cast<const T*>(at)); }
+// A cache that is read once: its lines are the first to leave the L2.  (Pays only where an instruction takes whole lines of 128 bytes: with half
+// lines, whose other half is asked for by the next instruction, they leave before that.)  Not where several units read the same rows.
+template <class T, bool kOnce>
+__device__ __forceinline__ T load_rows(const char* at) {
+  if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
+  return *reinterpret_cast<const T*>(at);
+}
 template <bool kBf16>
 __device__ __forceinline__ void store4(char* at, floatx4 o) {
   if constexpr (kBf16) {
@@ -100,8 +103,8 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
   }
 }
 
-// kSplit: the cut by runs.  Otherwise a workgroup per (sequence, run of query heads).
-template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit>
+// kSplit: the cut by runs.  Otherwise a workgroup per (sequence, run of query heads).  kOnce: rows are read by one unit.
+template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit, bool kOnce>
 __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
   constexpr int kHeads = 16 * kNT, kElem = kBf16 ? 2 : 4, kThreads = 64 * kWaves;
   constexpr int kKSteps = kD * kElem / 64;               // 16-byte chunks of a K row per lane
@@ -112,18 +115,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
   __shared__ int64_t row_at[kWaves][2][kDecodeTile];         // K, V
   float2* const part_ml = reinterpret_cast<float2*>(part + kWaves * a.part_heads * kPitch);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
-  const int per_seq = a.heads_kv * a.units;
+  const int per_seq = kSplit ? a.heads_kv : a.heads_kv * a.units;
 
   // the run of this workgroup and the sequence that its first place is of: every wave finds them for itself, a run of sequences to a lane
-  int b = 0, first = 0, run = 0, begin = 0, end = 1;
+  int b = 0, first = 0, run = 0, begin = 0, end = 1, group = 0, sub = 0;
   if constexpr (kSplit) {
     const int each = (a.batch + 63) / 64, i0 = min(lane * each, a.batch), i1 = min(i0 + each, a.batch);
     int mine = 0;
     for (int i = i0; i < i1; ++i) mine += decode_places(cached_tokens(a, i));
     const int upto = wave_scan(mine);
     const int total = __builtin_amdgcn_readlane(upto, 63) * per_seq;
-    run = decode_run(total);
-    begin = blockIdx.x * run;
+    run = decode_run(total * a.units);
+    group = blockIdx.x;
+    if (a.units > 1) {                          // those of the units of one run: at the same time on one XCD, whose L2 has the rows then
+      const int line = blockIdx.x / (8 * a.units), rest = blockIdx.x - line * 8 * a.units;
+      group = line * 8 + (rest & 7);
+      sub = rest >> 3;
+    }
+    begin = group * run;
     end = min(begin + run, total);
     if (begin >= total) return;
     const int seq_place = begin / per_seq;      // as if all heads lay side by side: places [seq_place, ..) of one head
@@ -136,22 +145,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       first += n;
     }
     first *= per_seq;
-    if (blockIdx.x == 0 && tid == 0) a.first_place[a.batch] = run;
+    if (begin == 0 && sub == 0 && tid == 0) a.first_place[a.batch] = run;
   } else {
     b = blockIdx.x / per_seq;
   }
 
   for (int pos = begin; pos < end;) {
     const int len = cached_tokens(a, b), seq = b;
-    int unit, t0 = 0, t1 = (len + kDecodeTile - 1) / kDecodeTile, place = 0;      // tiles
+    int kvh, t0 = 0, t1 = (len + kDecodeTile - 1) / kDecodeTile, place = 0;      // tiles
     bool whole = true;
     if constexpr (kSplit) {
       const int steps = decode_steps(len), seq_first = first;
-      unit = (pos - first) / (steps + kDecodeLead);
-      const int head_first = first + unit * (steps + kDecodeLead);
-      const DecodePiece piece = decode_piece(head_first, steps, blockIdx.x, run);
+      kvh = (pos - first) / (steps + kDecodeLead);
+      const int head_first = first + kvh * (steps + kDecodeLead);
+      const DecodePiece piece = decode_piece(head_first, steps, group, run);
       pos = head_first + steps + kDecodeLead;
-      if (unit + 1 == per_seq) {
+      if (kvh + 1 == per_seq) {
         ++b;
         first = pos;
       }
@@ -159,13 +168,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       t0 = piece.t0 * kDecodeWaves;
       t1 = min(t1, piece.t1 * kDecodeWaves);
       whole = piece.t0 == 0 && piece.t1 == steps;
-      place = decode_part(piece, blockIdx.x);
-      if (unit == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
+      place = decode_part(piece, group) * a.units + sub;
+      if (kvh == 0 && sub == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
     } else {
-      unit = blockIdx.x - b * per_seq;
+      const int unit = blockIdx.x - b * per_seq;
+      kvh = unit / a.units;
+      sub = unit - kvh * a.units;
       pos = end;
     }
-    const int kvh = unit / a.units, h0 = kvh * a.group + (unit - kvh * a.units) * kHeads;
+    const int h0 = kvh * a.group + sub * kHeads;
     const int heads = min(kHeads, (kvh + 1) * a.group - h0);
 
     // queries: lane (g, n) holds chunk 4 c + g of head n
@@ -214,7 +225,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
         for (int i = 0; i < 2; ++i) {         // rows 8 i .. 8 i + 7 of the half, a line of 128 bytes each
           const char* row = k_head + row_at[wave][0][16 * s + 8 * i + (r & 7)] + (r >> 3) * 64 + g * 16;
 #pragma unroll
-          for (int c = 0; c < kKSteps; c += 2) kf[s][c + i] = load_once<uintx4>(row + c * 64);
+          for (int c = 0; c < kKSteps; c += 2) kf[s][c + i] = load_rows<uintx4, kOnce>(row + c * 64);
         }
       uint32_t vf[2][4][kVLoads][4];
 #pragma unroll
@@ -225,10 +236,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
 #pragma unroll
           for (int u = 0; u < kVLoads; ++u) {
             if constexpr (kBf16 && kD == 64) {
-              const uintx2 w = load_once<uintx2>(row + r * 8);
+              const uintx2 w = load_rows<uintx2, kOnce>(row + r * 8);
               vf[s][j][u][0] = w[0]; vf[s][j][u][1] = w[1];
             } else {
-              const uintx4 w = load_once<uintx4>(row + r * 16 + u * 256);
+              const uintx4 w = load_rows<uintx4, kOnce>(row + r * 16 + u * 256);
 #pragma unroll
               for (int e = 0; e < 4; ++e) vf[s][j][u][e] = w[e];
             }
@@ -396,7 +407,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
   const int heads_q = a.heads_kv * a.group, id = min((int)blockIdx.x * kAtOnce + mine, a.batch * heads_q - 1), b = id / heads_q, head = id - b * heads_q;
   const int kvh = head / a.group, sub = (head - kvh * a.group) / heads_per_unit, h = head - kvh * a.group - sub * heads_per_unit;
   const int run = a.first_place[a.batch], steps = decode_steps(cached_tokens(a, b));
-  const int first = a.first_place[b] + (kvh * a.units + sub) * (steps + kDecodeLead);
+  const int first = a.first_place[b] + kvh * (steps + kDecodeLead);
   const int g0 = decode_first_group(first, run), g1 = decode_last_group(first, steps, run);
   const bool split = g0 != g1 && (kAtOnce == 1 || id == (int)blockIdx.x * kAtOnce + mine);
   if (kAtOnce == 1 && !split) return;
@@ -409,7 +420,7 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
 #pragma unroll
     for (int j = 0; j < kPartsAtOnce; ++j) {
       const int w = min(w0 + j * kRows, g1);
-      const int64_t place = (int64_t)decode_part(decode_piece(first, steps, w, run), w) * a.part_heads + h;
+      const int64_t place = (int64_t)(decode_part(decode_piece(first, steps, w, run), w) * a.units + sub) * a.part_heads + h;
       ml[j] = a.part_ml[place];
       p[j] = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
     }
@@ -447,7 +458,9 @@ __global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int head
   if (a.lse && c == 0) a.lse[id] = lse_of(top, sum, a.scale);
 }
 
-// Query heads that share the loads of their KV head: up to 32 (bf16), 16 (f32, whose rows take twice the registers).
+// Query heads that share the loads of their KV head, a unit: up to 32 (bf16), 16 (f32, whose rows take twice the registers).  Of more heads there
+// are several units, whose workgroups read the rows at the same time through one L2: 64 sequences of 16384 tokens, 64 heads on 1, bf16 205 -> 148 us (each
+// unit by itself -> side by side, rows kept); 16 of 8192, 160 heads on 8, f32 373 -> 291; 320 heads 545 -> 377.
 int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
 // One workgroup of 8 waves for all of a (sequence, run of query heads): no cut, no join, one launch.  A compute unit takes in some 64 GB/s, 2.2 us
 // for 256 tokens of bf16, d = 128, whatever its waves do; so that is for calls that are short, or have a workgroup for every compute unit and are
@@ -462,6 +475,8 @@ bool has_small_workgroups(int64_t units, int row_tokens) { return units >= 2 * r
 int64_t most_places(int batch, int heads_kv, int group, bool bf16, int row_tokens) {
   return (int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens);
 }
+// Runs of a call, whatever the lengths turn out to be; as many workgroups for each as there are units.
+int most_runs(int64_t places, int units) { return ceil_div(decode_groups(places), units); }
 struct DecodeWs { size_t first_place, part_o, part_ml, total; };
 DecodeWs carve(int batch, int groups, int part_heads, int d) {
   DecodeWs w;
@@ -473,9 +488,9 @@ DecodeWs carve(int batch, int groups, int part_heads, int d) {
   return w;
 }
 
-template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit>
+template <bool kBf16, int kD, int kNT, int kWaves, bool kSplit, bool kOnce = true>
 basa_status launch_kernel(const DecodeArgs& a, int groups, hipStream_t st) {
-  const auto kernel = decode_kernel<kBf16, kD, kNT, kWaves, kSplit>;
+  const auto kernel = decode_kernel<kBf16, kD, kNT, kWaves, kSplit, kOnce>;
   const int lds = kWaves * a.part_heads * ((kD + 4) * 4 + 8);
   if (lds > 60 * 1024) {
     const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -491,7 +506,10 @@ basa_status launch(const DecodeArgs& a, int groups, hipStream_t st) {
   const int64_t units = (int64_t)a.batch * a.heads_kv * a.units;
   if (is_solo(units, a.row_tokens) && has_small_workgroups(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 2, false>(a, (int)units, st);
   if (is_solo(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 8, false>(a, (int)units, st);
-  const basa_status s = launch_kernel<kBf16, kD, kNT, kDecodeWaves, true>(a, groups, st);
+  basa_status s;
+  if constexpr (!kBf16 || kNT > 1) s = a.units > 1 ? launch_kernel<kBf16, kD, kNT, kDecodeWaves, true, false>(a, groups, st)
+                                                   : launch_kernel<kBf16, kD, kNT, kDecodeWaves, true>(a, groups, st);
+  else s = launch_kernel<kBf16, kD, kNT, kDecodeWaves, true>(a, groups, st);
   if (s != BASA_OK) return s;
   ProfScope prof(K_DECODE_JOIN, st);
   const int rows = a.batch * a.heads_kv * a.group;
@@ -509,7 +527,8 @@ bool decode_takes(int batch, int heads_q, int heads_kv, bool bf16, int row_token
 size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool bf16, int row_tokens) {
   const int group = heads_q / heads_kv;
   if (is_solo((int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)), row_tokens)) return 256;
-  return carve(batch, decode_groups(most_places(batch, heads_kv, group, bf16, row_tokens)), std::min(group, heads_per_unit(group, bf16)), d).total;
+  const int hpu = heads_per_unit(group, bf16), units = ceil_div(group, hpu);
+  return carve(batch, most_runs(most_places(batch, heads_kv, group, bf16, row_tokens), units) * units, std::min(group, hpu), d).total;
 }
 
 basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
@@ -529,9 +548,10 @@ basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, c
   const int hpu = heads_per_unit(a.group, bf16);
   a.units = ceil_div(a.group, hpu);
   a.out = static_cast<char*>(out); a.out_b = out_sb * e; a.out_h = out_sh * e; a.lse = lse;
-  const int groups = decode_groups(most_places(a.batch, a.heads_kv, a.group, bf16, a.row_tokens));
+  const int runs = most_runs(most_places(a.batch, a.heads_kv, a.group, bf16, a.row_tokens), a.units);
+  const int groups = a.units == 1 ? runs : (int)align_up(runs, 8) * a.units;
   a.part_heads = std::min(a.group, hpu);
-  const DecodeWs w = carve(a.batch, groups, a.part_heads, q.d);
+  const DecodeWs w = carve(a.batch, runs * a.units, a.part_heads, q.d);
   char* base = static_cast<char*>(ws);
   a.first_place = reinterpret_cast<int*>(base + w.first_place);
   a.part_o = reinterpret_cast<float*>(base + w.part_o);
