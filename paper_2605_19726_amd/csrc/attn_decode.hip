@@ -394,13 +394,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
   }
 }
 
-// The pieces of a (sequence, query head) that more than one workgroup had a part in, added up: a workgroup per sequence and head, 4 numbers to
-// a lane, every 256 / (d / 4)-th part to a lane group, four of them requested at once.
-// With many rows, whose sequences are cut into few parts if at all, a wave takes one and a workgroup four.
+// The pieces of a (sequence, query head) that more than one workgroup had a part in, added up: 4 numbers to a lane, a part to every d / 4
+// lanes, four of them requested at once.  kThreads to a row: 1024 where there are few rows, whose sequences may be cut into hundreds of
+// parts; 64, four rows to a workgroup, where there are many, whose sequences are cut into few if at all.
 constexpr int kPartsAtOnce = 4, kCUs = 256;
-template <bool kBf16, int kD, int kAtOnce>
-__global__ __launch_bounds__(256) void decode_join_kernel(DecodeArgs a, int heads_per_unit) {
-  constexpr int kLanes = kD / 4, kThreads = 256 / kAtOnce, kRows = kThreads / kLanes, kElem = kBf16 ? 2 : 4;
+template <bool kBf16, int kD, int kThreads>
+__global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void decode_join_kernel(DecodeArgs a, int heads_per_unit) {
+  constexpr int kAtOnce = kThreads < 256 ? 256 / kThreads : 1, kLanes = kD / 4, kRows = kThreads / kLanes, kElem = kBf16 ? 2 : 4;
   __shared__ floatx4 row_o[kAtOnce][kRows][kLanes];
   __shared__ float2 row_ml[kAtOnce][kRows];
   const int tid = threadIdx.x % kThreads, mine = threadIdx.x / kThreads;
@@ -513,8 +513,9 @@ basa_status launch(const DecodeArgs& a, int groups, hipStream_t st) {
   if (s != BASA_OK) return s;
   ProfScope prof(K_DECODE_JOIN, st);
   const int rows = a.batch * a.heads_kv * a.group;
-  if (rows < 4 * kCUs) decode_join_kernel<kBf16, kD, 1><<<rows, 256, 0, st>>>(a, 16 * kNT);
-  else decode_join_kernel<kBf16, kD, 4><<<ceil_div(rows, 4), 256, 0, st>>>(a, 16 * kNT);
+  if (rows <= kCUs) decode_join_kernel<kBf16, kD, 1024><<<rows, 1024, 0, st>>>(a, 16 * kNT);
+  else if (rows < 4 * kCUs) decode_join_kernel<kBf16, kD, 256><<<rows, 256, 0, st>>>(a, 16 * kNT);
+  else decode_join_kernel<kBf16, kD, 64><<<ceil_div(rows, 4), 256, 0, st>>>(a, 16 * kNT);
   BASA_HIP_CHECK_LAUNCH("decode_join_kernel");
   return BASA_OK;
 }
