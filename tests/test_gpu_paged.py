@@ -189,7 +189,7 @@ def test_decode_against_64_bits(dtype, d, hq, hk, page, layout):
 
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("hq,hk,lens", [(4, 1, [70001]), (8, 2, [20000, 3, 9999]), (2, 2, [40000, 0, 1, 64, 33333]), (20, 1, [30011, 17]),
-                                        (48, 1, [5000])])
+                                        (48, 1, [5000]), (128, 1, [20000, 5, 2000]), (68, 2, [1500] * 9)])
 def test_long_sequences_are_split_and_joined(dtype, hq, hk, lens):
     q, k, v, table = _decode_case(dtype, 128, hq, hk, 64, lens, 3)
     cache = bd.PagedCache(k, v)
@@ -200,7 +200,7 @@ def test_long_sequences_are_split_and_joined(dtype, hq, hk, lens):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-@pytest.mark.parametrize("n", [256, 700, 3001])
+@pytest.mark.parametrize("n", [256, 512, 513, 700, 3001])
 def test_many_short_sequences(dtype, n):
     lens = np.random.default_rng(n).integers(0, 70, n)
     lens[n // 2] = 3000
