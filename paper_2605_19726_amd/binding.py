@@ -430,6 +430,10 @@ class PagedCache:
             raise ValueError("keys and values must agree in shape, dtype and device")
         self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
         self.pages, self.heads, self.page, self.d = k.shape
+        for desc in (self._kd, self._vd):        # (the stride of an axis of one means nothing)
+            desc.stride_b = desc.stride_b if self.pages > 1 else 0
+            desc.stride_h = desc.stride_h if self.heads > 1 else 0
+            desc.stride_l = desc.stride_l if self.page > 1 else self.d
         self._keys = C.byref(self._kd), C.byref(self._vd)
 
 
@@ -551,7 +555,8 @@ def decode_workspace_size(q, cache: PagedCache, table) -> int:
 
 
 def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, ws=None, out=None):
-    """Attention of one new token of every sequence, q [batch, heads_q, d], over the first lens[i] tokens of its pages."""
+    """Attention of one new token of every sequence, q [batch, heads_q, d], over the first lens[i] tokens of its pages.  The launch is sized by
+    the table's width: table[:, :w] with the columns in use is faster than a table with room for the longest context there is."""
     lib, dev = load(), cache.device
     qd = _token_desc(q, "q", cache)
     b, hq, d = q.shape
@@ -582,7 +587,8 @@ def ba_att_decode(q, k, v, cache: PagedCache, table, lens, slots, want_lse: bool
 def ba_att_cached(q, k, v, cu_seqlens, cache: PagedCache, table, slots, cached=None, block: int = 128, sparsity: float = 0.5, **kw):
     """ba_att_varlen over a packed batch of prompts whose keys and values enter the cache: sequence i has rows cu_seqlens[i] ..
     cu_seqlens[i + 1] - 1 (host list) of q, k and v.  cached: host list of the tokens that a sequence held before; its new queries then meet
-    all of them, read back from the pages, and the new ones (`causal` counts from the end: the last query sees every key)."""
+    all of them, read back from the pages, and the new ones (`causal` counts from the end: the last query sees every key).  Every sequence has to
+    have its slots: what basa_page_tables did not serve is not in the pages."""
     cu = [int(t) for t in cu_seqlens]
     before = [0] * (len(cu) - 1) if cached is None else [int(t) for t in cached]
     if len(before) != len(cu) - 1 or any(t < 0 for t in before):

@@ -423,3 +423,74 @@ def test_prompts_then_steps_then_a_prompt_that_goes_on(dtype, d, hq, hk, page, l
         want, _ = bd.ba_att(view(q[part]), view(held[i][0]), view(held[i][1]), block, 0.5, causal=True)
         assert torch.equal(view(out[part]), want)
     assert table.max() < 150 and len(set(table[table >= 0].tolist())) == int((table >= 0).sum()) == used
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_captured_step_replays_on_its_own_results(dtype):
+    """Tables, append and attention of a decode step in one graph that feeds its lengths and its free pages back to itself."""
+    page, hk, hq, d, width, total = 16, 2, 8, 64, 80, 400
+    start = [15, 0, 1000, 47]
+    n = len(start)
+    q, k_cache, v_cache, held = _decode_case(dtype, d, hq, hk, page, start, 91, spare=total - sum(-(-x // page) for x in start))
+    table = np.full((n, width), -1, dtype=np.int32)
+    table[:, :held.shape[1]] = held
+    pool = np.setdiff1d(np.arange(total), table[table >= 0]).astype(np.int32)
+    cache, tab, have, one = bd.PagedCache(k_cache, v_cache), ints(table), ints(start), ints([1] * n)
+    pool_d, used = ints(pool), ints([0], torch.int64)
+    free, ar = pool_d[:n].clone(), torch.arange(n, device=DEV)
+    plan, out = bd.PageTables(n, n + 2, DEV), torch.empty_like(q)
+    k, v = randn((n + 2, hk, d), 1, dtype), randn((n + 2, hk, d), 2, dtype)          # two rows of padding
+    ws = torch.empty(bd.decode_workspace_size(q, cache, tab), dtype=torch.uint8, device=DEV)
+
+    def step():
+        bd.basa_page_tables(have, one, tab, free, page, n + 2, out=plan)
+        bd.basa_cache_append(k, v, plan.slots, cache)
+        bd.basa_decode_attn(q, cache, tab, plan.lens, ws=ws, out=out)
+        have.copy_(plan.lens)
+        used.add_(plan.pages[0])
+        free.copy_(pool_d[used + ar])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    state = [x.clone() for x in (tab, have, used, free, k_cache, v_cache)]
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    for x, y in zip((tab, have, used, free, k_cache, v_cache), state):
+        x.copy_(y)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    lens, given = list(start), 0
+    for it in range(20):
+        for x, seed in ((q, 3), (k, 1), (v, 2)):
+            x.copy_(randn(x.shape, 1000 * it + seed, dtype))
+        out.fill_(9.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        want, slots, after, _, pages = page_tables(lens, [1] * n, table, pool[given:given + n], page, n + 2)
+        given += int(pages[0])
+        lens, table = after.tolist(), want
+        assert np.array_equal(tab.cpu().numpy(), want) and np.array_equal(plan.slots.cpu().numpy(), slots) and have.tolist() == lens
+        at, off = torch.from_numpy(slots[:n] // page).to(DEV), torch.from_numpy(slots[:n] % page).to(DEV)
+        assert torch.equal(k_cache[at, :, off], k[:n]) and torch.equal(v_cache[at, :, off], v[:n])
+        check_decode(out, None, q, k_cache, v_cache, want, lens, f"replay {it}")
+        assert torch.equal(out, bd.basa_decode_attn(q, cache, tab, plan.lens))
+    assert len(set(table[table >= 0].tolist())) == int((table >= 0).sum())
+
+
+def test_calls_on_two_streams_with_workspaces_of_their_own():
+    lens = [3000, 10, 0, 900]
+    q, k, v, table = _decode_case(BF, 128, 8, 2, 16, lens, 95)
+    cache, tab, now = bd.PagedCache(k, v), ints(table), ints(lens)
+    want = bd.basa_decode_attn(q, cache, tab, now)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [[], []]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for _ in range(10):
+        for s, o in zip(streams, outs):
+            with torch.cuda.stream(s):
+                o.append(bd.basa_decode_attn(q, cache, tab, now))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for side in outs for o in side)

@@ -83,6 +83,7 @@ def test_decode(lib):  # noqa: F811
     assert call(q=query(d=96), kp=pages(d=96), vp=pages(d=96)) == UNSUPPORTED
     assert call(width=2 ** 27, stride=2 ** 27) == UNSUPPORTED
     assert call(q=query(batch=2 ** 28)) == UNSUPPORTED
+    assert call(q=query(batch=100), width=2 ** 26, stride=2 ** 26) == UNSUPPORTED and b"steps" in lib.basa_last_error()
     size = lambda q, kp, w: lib.basa_decode_workspace_size(C.byref(q), C.byref(kp), C.byref(kp), w)
     need = size(query(), pages(), 8)
     assert need > 0 and call(n=need - 1) == WORKSPACE and call(ws=None) == WORKSPACE and b"need" in lib.basa_last_error()
@@ -117,3 +118,38 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
                 lambda: bd.ba_att_cached(rows, rows, rows, [0, 5], cache, table, slots, cached=[1, 2])):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_calls_go_to_the_device_of_their_tensors(monkeypatch):
+    class Elsewhere:
+        device = torch.device("cuda", 1)
+
+    current, seen = [0], []
+
+    class Device:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            current.append(self.index)
+
+        def __exit__(self, *exc):
+            current.pop()
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[-1])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(bd, "_stream", lambda x: ("stream of", x.device.index))
+    bd._launch(lambda *args: seen.append((current[-1], args)) or 0, Elsewhere(), 5)
+    assert seen == [(1, (5, ("stream of", 1)))] and current == [0]
+
+
+def test_strides_of_axes_of_one_do_not_count():
+    one = torch.zeros(64, dtype=torch.bfloat16)
+    x = one.as_strided((1, 1, 1, 64), (3, 5, 7, 1))
+    cache = bd.PagedCache(x, x)
+    assert (cache._kd.stride_b, cache._kd.stride_h, cache._kd.stride_l) == (0, 0, 64)
+    row = one.as_strided((1, 1, 64), (3, 5, 1))
+    desc = bd._packed_desc(row, "k", cache)
+    assert desc.stride_h == 0 and desc.stride_l >= 64
+    desc = bd._token_desc(row, "q", cache)
+    assert (desc.stride_b, desc.stride_h, desc.stride_l) == (0, 0, 64)
