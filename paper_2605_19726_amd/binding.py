@@ -184,9 +184,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()             # (the prototypes turn it into a pointer)
 
 
+# What torch.cuda.current_stream(device).cuda_stream and torch.cuda.current_device() give, without the Stream object (2 us a call) and the check
+# that the device is initialised (tensors on it are in hand).
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+
+
 def _stream(x: torch.Tensor):
-    # (the handle of torch.cuda.current_stream(x.device) without the Stream object, which costs 2 us a call)
-    return torch._C._cuda_getCurrentRawStream(x.device.index)
+    return _raw_stream(x.device.index)
 
 
 def _ws(nbytes: int, device) -> torch.Tensor:
@@ -422,7 +427,7 @@ def _varlen_params(block, sparsity, beta: float = 1.0, sort: int = SORT_QK, wind
 class PagedCache:
     """Keys and values in pages, indexed [pages, heads_kv, page, d]: the two tensors and their descriptors.  Any strides with a
     contiguous d axis (a token-major store [pages, page, heads_kv, d] comes as its permute(0, 2, 1, 3))."""
-    __slots__ = ("k", "v", "device", "dtype", "pages", "heads", "page", "d", "_kd", "_vd", "_keys")
+    __slots__ = ("k", "v", "device", "dtype", "pages", "heads", "page", "d", "_kd", "_vd")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
         self._kd, self._vd = tensor_desc(k), tensor_desc(v)
@@ -434,7 +439,6 @@ class PagedCache:
             desc.stride_b = desc.stride_b if self.pages > 1 else 0
             desc.stride_h = desc.stride_h if self.heads > 1 else 0
             desc.stride_l = desc.stride_l if self.page > 1 else self.d
-        self._keys = C.byref(self._kd), C.byref(self._vd)
 
 
 class PageTables:
@@ -481,13 +485,14 @@ def _packed_desc(x: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
     return BasaTensor(x.data_ptr(), cache._kd.dtype, 1, h, T, d, 0, sh if h > 1 else 0, st if T > 1 else max(d, st))
 
 
-def _launch(entry, x: torch.Tensor, *args):
-    """A library call on the current stream of x's device, with that device as the current one (its launches go there)."""
-    if x.device.index == torch.cuda.current_device():
-        status = entry(*args, _stream(x))
+def _launch(entry, device, *args):
+    """A library call on the device's current stream, with that device as the current one (its launches go there)."""
+    index = device.index
+    if index == _current_device():
+        status = entry(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(x.device):
-            status = entry(*args, _stream(x))
+        with torch.cuda.device(index):
+            status = entry(*args, _raw_stream(index))
     if status != BASA_OK:
         _check(status)
 
@@ -504,7 +509,7 @@ def basa_page_tables(have, add, table, free_pages, page: int, tokens: int, out: 
     slots, lens, cu, pages = out._ptrs
     args = (_int_array(have, "have", dev, (n,)), _int_array(add, "add", dev, (n,)), n, int(page), tab, width, stride,
             _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0], slots, int(tokens), lens, cu, pages)
-    _launch(lib.basa_page_tables, table, *args)
+    _launch(lib.basa_page_tables, dev, *args)
     return out
 
 
@@ -516,7 +521,7 @@ def basa_cache_append(k, v, slots, cache: PagedCache):
     at = _int_array(slots, "slots", cache.device, k.shape[:1], torch.int64)
     if k.shape[0] == 0:
         return
-    _launch(load().basa_cache_append, k, C.byref(kd), C.byref(vd), at, *cache._keys)
+    _launch(load().basa_cache_append, cache.device, kd, vd, at, cache._kd, cache._vd)
 
 
 def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=None):
@@ -533,7 +538,7 @@ def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=Non
     if k.shape[0] != tokens or v.shape != k.shape:
         raise ValueError("out: two tensors of `tokens` rows")
     if tokens:
-        _launch(load().basa_cache_gather, k, *cache._keys, tab, width, stride, cu, n, C.byref(kd), C.byref(vd))
+        _launch(load().basa_cache_gather, cache.device, cache._kd, cache._vd, tab, width, stride, cu, n, kd, vd)
     return k, v
 
 
@@ -551,7 +556,7 @@ _TwoStrides = C.c_int64 * 2
 
 def decode_workspace_size(q, cache: PagedCache, table) -> int:
     """Bytes of workspace for basa_decode_attn with tables of this width."""
-    return int(load().basa_decode_workspace_size(C.byref(_token_desc(q, "q", cache)), *cache._keys, table.shape[1]))
+    return int(load().basa_decode_workspace_size(_token_desc(q, "q", cache), cache._kd, cache._vd, table.shape[1]))
 
 
 def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, ws=None, out=None):
@@ -568,12 +573,11 @@ def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, 
         raise ValueError("out must have the shape, dtype and device of q and a contiguous d axis")
     lse = torch.empty((b, hq), dtype=torch.float32, device=dev) if want_lse else None
     if b:
-        qr = C.byref(qd)
         if ws is None:
-            ws = _ws(lib.basa_decode_workspace_size(qr, *cache._keys, width), dev)
+            ws = _ws(lib.basa_decode_workspace_size(qd, cache._kd, cache._vd, width), dev)
         sb, sh, _ = out.stride()
         ostr = _TwoStrides(sb if b > 1 else 0, sh if hq > 1 else d)
-        _launch(lib.basa_decode_attn, q, qr, *cache._keys, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel())
+        _launch(lib.basa_decode_attn, dev, qd, cache._kd, cache._vd, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel())
     return (out, lse) if want_lse else out
 
 

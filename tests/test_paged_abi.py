@@ -121,14 +121,11 @@ def test_the_binding_refuses_what_the_kernels_would_misread():
 
 
 def test_calls_go_to_the_device_of_their_tensors(monkeypatch):
-    class Elsewhere:
-        device = torch.device("cuda", 1)
-
     current, seen = [0], []
 
     class Device:
-        def __init__(self, device):
-            self.index = device.index
+        def __init__(self, index):
+            self.index = index
 
         def __enter__(self):
             current.append(self.index)
@@ -136,11 +133,12 @@ def test_calls_go_to_the_device_of_their_tensors(monkeypatch):
         def __exit__(self, *exc):
             current.pop()
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[-1])
+    monkeypatch.setattr(bd, "_current_device", lambda: current[-1])
     monkeypatch.setattr(torch.cuda, "device", Device)
-    monkeypatch.setattr(bd, "_stream", lambda x: ("stream of", x.device.index))
-    bd._launch(lambda *args: seen.append((current[-1], args)) or 0, Elsewhere(), 5)
-    assert seen == [(1, (5, ("stream of", 1)))] and current == [0]
+    monkeypatch.setattr(bd, "_raw_stream", lambda index: ("stream of", index))
+    for index in (1, 0):
+        bd._launch(lambda *args: seen.append((current[-1], args)) or 0, torch.device("cuda", index), 5)
+    assert seen == [(1, (5, ("stream of", 1))), (0, (5, ("stream of", 0)))] and current == [0]
 
 
 def test_strides_of_axes_of_one_do_not_count():
