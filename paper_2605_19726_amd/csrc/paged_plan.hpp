@@ -37,11 +37,11 @@ constexpr int kDecodeLead = 1;
 BASA_HD int decode_steps(int len) { return len <= kDecodeStep ? 1 : (len + kDecodeStep - 1) / kDecodeStep; }
 BASA_HD int decode_places(int len) { return decode_steps(len) + kDecodeLead; }
 // The length of a run: two workgroups fit a compute unit, so short rows are cut into as many runs as there is room for at once.  Where
-// those would be longer than 24 steps there are more, down to 8 steps, so that a workgroup that is done early is followed by another; 3072
+// those would be longer than 24 steps there are more, down to 8 steps, so that a workgroup that is done early is followed by another; 2048
 // at most, which is as far as that helps.  Main kernel + join, one round -> runs of 8 and more: 1024 (sequence, head) of 2000 tokens, d = 128:
 // 205 + 4 -> 167 + 4 us; 2048 of 100 to 4000: 218 + 10.5 -> 185 + 11; one sequence of 128K tokens, 8 heads (17 steps): 86 + 5.8, in runs
 // of 8 89 + 9.3.
-constexpr int kDecodeOneRound = 512, kDecodeMost = 3072, kDecodeLongRun = 24, kDecodeShortRun = 8;
+constexpr int kDecodeOneRound = 512, kDecodeMost = 2048, kDecodeLongRun = 24, kDecodeShortRun = 8;
 BASA_HD int decode_run(int total) {          // total < 2^31 - kDecodeMost
   const int one = (total + kDecodeOneRound - 1) / kDecodeOneRound, many = (total + kDecodeMost - 1) / kDecodeMost;
   return one <= kDecodeLongRun ? one : many > kDecodeShortRun ? many : kDecodeShortRun;

@@ -86,3 +86,14 @@ def test_runs_take_every_step_once_and_give_every_piece_a_place_of_its_own(plan)
                 assert place not in places and place // 2 == g < groups
                 places.add(place)
         assert done == steps
+
+
+def test_a_launch_has_a_workgroup_for_every_run_of_several_units(plan):
+    """Units of query heads share the places; the length of a run goes by places times units, the launch by the most there can be."""
+    rng = random.Random(3)
+    totals = [1, 2, 511, 512, 513, 12287, 12288, 12289, 16384, 16385, 10 ** 6, 10 ** 8] + [int(2 ** rng.uniform(0, 27)) for _ in range(200)]
+    for units in (1, 2, 3, 4, 7):
+        runs = plan([("run", t * units) for t in totals])
+        groups = plan([("groups", t * units) for t in totals])
+        for t, run, g in zip(totals, runs, groups):
+            assert -(-t // run) <= -(-g // units), (t, units, run, g)
