@@ -531,12 +531,15 @@ def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=Non
     tab, width, stride = _block_table(table, n, cache.device)
     cu = _int_array(cu_seqlens, "cu_seqlens", cache.device, (n + 1,))
     if out is None:
-        shape = (int(tokens), cache.heads, cache.d)
-        out = tuple(torch.empty(shape, dtype=cache.dtype, device=cache.device) for _ in range(2))
-    k, v = out
-    kd, vd = _packed_desc(k, "k", cache), _packed_desc(v, "v", cache)
-    if k.shape[0] != tokens or v.shape != k.shape:
-        raise ValueError("out: two tensors of `tokens` rows")
+        T, h, d = int(tokens), cache.heads, cache.d
+        k = torch.empty(T, h, d, dtype=cache.dtype, device=cache.device)
+        v = torch.empty_like(k)
+        kd, vd = (BasaTensor(x.data_ptr(), cache._kd.dtype, 1, h, T, d, 0, d, h * d) for x in (k, v))
+    else:
+        k, v = out
+        kd, vd = _packed_desc(k, "k", cache), _packed_desc(v, "v", cache)
+        if k.shape[0] != tokens or v.shape != k.shape:
+            raise ValueError("out: two tensors of `tokens` rows")
     if tokens:
         _launch(load().basa_cache_gather, cache.device, cache._kd, cache._vd, tab, width, stride, cu, n, kd, vd)
     return k, v
@@ -568,13 +571,15 @@ def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, 
     tab, width, stride = _block_table(table, b, dev)
     at = _int_array(lens, "lens", dev, (b,))
     if out is None:
-        out = torch.empty((b, hq, d), dtype=q.dtype, device=dev)
+        out = torch.empty(b, hq, d, dtype=q.dtype, device=dev)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or out.stride(2) != 1:
         raise ValueError("out must have the shape, dtype and device of q and a contiguous d axis")
-    lse = torch.empty((b, hq), dtype=torch.float32, device=dev) if want_lse else None
+    lse = torch.empty(b, hq, dtype=torch.float32, device=dev) if want_lse else None
     if b:
         if ws is None:
             ws = _ws(lib.basa_decode_workspace_size(qd, cache._kd, cache._vd, width), dev)
+        elif ws.device != dev:
+            raise ValueError(f"ws must be on {dev}")
         sb, sh, _ = out.stride()
         ostr = _TwoStrides(sb if b > 1 else 0, sh if hq > 1 else d)
         _launch(lib.basa_decode_attn, dev, qd, cache._kd, cache._vd, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel())
