@@ -336,7 +336,8 @@ basa_status basa_cache_gather(const basa_tensor* k_pages, const basa_tensor* v_p
 /*
  * Attention (Eq. 1) of one new token of every sequence over the first lens[i] tokens of its pages (the new one among them, once it was
  * appended), all of them: what the block-sparse prefill of a prompt is followed by.
- *   q            [batch, heads_q, 1, d]; sequence i is batch entry i.  Query head h reads KV head h / (heads_q / heads_kv).
+ *   q            [batch, heads_q, 1, d], batch * heads_q up to 2^22; sequence i is batch entry i.  Query head h reads KV head
+ *                h / (heads_q / heads_kv).
  *   width        entries of a table row that may be in use: the launch is sized by them.  batch * heads_kv, times the runs of 32 (f32: 16) query
  *                heads that share one, times width * page / 128 has to stay below 2^31 (BASA_ERR_UNSUPPORTED).
  *   lens         [batch] int32; lengths below 0 count as 0, lengths beyond width * page as that.

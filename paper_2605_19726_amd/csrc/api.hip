@@ -352,7 +352,7 @@ basa_status check_varlen(const basa_tensor* q, const basa_tensor* k, const basa_
 
 // ---- paged key-value cache ------------------------------------------------------------------
 // Largest counts that the kernels take as 32-bit numbers with room for a step beyond them.
-constexpr int kMaxPagedTokens = 1 << 30;
+constexpr int kMaxPagedTokens = 1 << 30, kMaxDecodeRows = 1 << 22;
 
 basa_status check_pages(const basa_tensor* k, const basa_tensor* v) {
   basa_status s;
@@ -365,17 +365,20 @@ basa_status check_pages(const basa_tensor* k, const basa_tensor* v) {
   return BASA_OK;
 }
 // A block table of n_seq rows of `width` page ids, for pages of `page` tokens.
-basa_status check_table(const int32_t* table, int32_t n_seq, int32_t width, int64_t table_stride, int32_t page) {
-  if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
-  if (!table && n_seq > 0) { set_error("null block table"); return BASA_ERR_INVALID_ARG; }
-  if (width < 1 || table_stride < width) {
-    set_error("a block table needs width >= 1 and a row stride >= width (got %d, %lld)", width, (long long)table_stride);
-    return BASA_ERR_INVALID_ARG;
-  }
+basa_status check_width(int32_t width, int32_t page) {
+  if (width < 1) { set_error("a block table needs width >= 1 (got %d)", width); return BASA_ERR_INVALID_ARG; }
   if ((int64_t)width * page > kMaxPagedTokens) {
     set_error("block table rows of %d pages of %d tokens exceed %d tokens", width, page, kMaxPagedTokens); return BASA_ERR_UNSUPPORTED;
   }
   return BASA_OK;
+}
+basa_status check_table(const int32_t* table, int32_t n_seq, int32_t width, int64_t table_stride, int32_t page) {
+  if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
+  if (!table && n_seq > 0) { set_error("null block table"); return BASA_ERR_INVALID_ARG; }
+  if (table_stride < width) {
+    set_error("rows of the block table are %lld entries apart, %d wide", (long long)table_stride, width); return BASA_ERR_INVALID_ARG;
+  }
+  return check_width(width, page);
 }
 // Packed rows of k and v next to the pages that they come from or go to.
 basa_status check_packed(const basa_tensor* k, const basa_tensor* v, const basa_tensor* k_pages, const basa_tensor* v_pages) {
@@ -405,9 +408,8 @@ basa_status check_decode(const basa_tensor* q, const basa_tensor* k, const basa_
   if (q->heads % k->heads != 0) {
     set_error("query heads (%d) must be a multiple of kv heads (%d)", q->heads, k->heads); return BASA_ERR_INVALID_ARG;
   }
-  if ((int64_t)q->batch * q->heads > kMaxPagedTokens) { set_error("q: batch*heads exceeds %d", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
-  static const int32_t some = 0;
-  if ((s = check_table(&some, q->batch, width, width, k->L)) != BASA_OK) return s;
+  if ((int64_t)q->batch * q->heads > kMaxDecodeRows) { set_error("q: batch*heads exceeds %d", kMaxDecodeRows); return BASA_ERR_UNSUPPORTED; }
+  if ((s = check_width(width, k->L)) != BASA_OK) return s;
   if (!decode_takes(q->batch, q->heads, k->heads, q->dtype == BASA_BF16, width * k->L)) {
     set_error("%d sequences of %d KV heads with room for %lld tokens each: more steps than a call takes", q->batch, k->heads,
               (long long)width * k->L);

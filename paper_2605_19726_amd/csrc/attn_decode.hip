@@ -55,17 +55,7 @@ struct DecodeArgs {
 // sequences of 1 to 1100 tokens 22 us, 600 21.4 -> 4.2 + 19.9, 1000 of 1500 148 -> 4.0 + 139, 4000 of 1 to 2000 163 -> 4.3 + 120.
 constexpr int kPlanBatch = 512;
 __device__ __forceinline__ int cached_tokens(const DecodeArgs& a, int b) { return min(max(a.lens[b], 0), a.row_tokens); }
-// Sum over this lane and the ones before it.
-__device__ __forceinline__ int wave_scan(int x) {
-  constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
-  x += __builtin_amdgcn_update_dpp(0, x, kRowShr1, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, kRowShr2, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, kRowShr4, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, kRowShr8, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, kRowBcast15, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, kRowBcast31, 0xc, 0xf, false);
-  return x;
-}
+__device__ __forceinline__ int sum_of(int x, int y) { return x + y; }
 __device__ __forceinline__ float column_max(float v) {      // over the four lane groups
   uint32_t x, y;
   lane_pair<32>(__float_as_uint(v), x, y);
@@ -138,7 +128,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
         places[i] = i < each && at < a.batch ? n : 0;
         mine += places[i];
       }
-      const int upto = wave_scan(mine), total = __builtin_amdgcn_readlane(upto, 63) * per_seq;
+      const int upto = (int)wave_scan((uint32_t)mine, sum_of), total = __builtin_amdgcn_readlane(upto, 63) * per_seq;
       run = decode_run(total * a.units);
       begin = group * run;
       end = min(begin + run, total);
@@ -427,7 +417,7 @@ __global__ __launch_bounds__(1024) void decode_plan_kernel(DecodeArgs a) {
   const int tid = threadIdx.x, each = (a.batch + 1023) / 1024, i0 = min(tid * each, a.batch), i1 = min(i0 + each, a.batch);
   int mine = 0;
   for (int i = i0; i < i1; ++i) mine += decode_places(cached_tokens(a, i));
-  const int upto = wave_scan(mine);
+  const int upto = (int)wave_scan((uint32_t)mine, sum_of);
   if ((tid & 63) == 63) wave_sum[tid >> 6] = upto;
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();

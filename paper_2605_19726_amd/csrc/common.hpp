@@ -309,6 +309,17 @@ __device__ __forceinline__ float wave_reduce(float v, Op op) {
   v = op(v, __uint_as_float(lane_xor<2>(__float_as_uint(v))));
   return op(v, __uint_as_float(lane_xor<1>(__float_as_uint(v))));
 }
+// op over this lane and the lanes before it (0 is its neutral element).
+template <class Op>
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x, Op op) {
+  constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowShr1, 0xf, 0xf, false));
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowShr2, 0xf, 0xf, false));
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowShr4, 0xf, 0xf, false));
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowShr8, 0xf, 0xf, false));
+  x = op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowBcast15, 0xa, 0xf, false));
+  return op(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kRowBcast31, 0xc, 0xf, false));
+}
 // Entry `pos` of a permutation of 0..L-1 (null = identity).  Permutations are device data the
 // host cannot check: a value that is no index falls back to `pos`, so that a malformed
 // permutation gives wrong rows, never an access outside the tensor.

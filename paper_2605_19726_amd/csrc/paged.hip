@@ -14,18 +14,11 @@ __device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return __b
 // Running sum over the threads of a workgroup of 256: the sum of the values of all threads before this one; *all: of every thread.  An array
 // serves one call.
 __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* all, uint32_t (&wave_sum)[4]) {
-  constexpr int kRowShr1 = 0x111, kRowShr2 = 0x112, kRowShr4 = 0x114, kRowShr8 = 0x118, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
   constexpr int kWaveShr1 = 0x138;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t x = v;
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowShr1, 0xf, 0xf, false));
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowShr2, 0xf, 0xf, false));
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowShr4, 0xf, 0xf, false));
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowShr8, 0xf, 0xf, false));
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowBcast15, 0xa, 0xf, false));
-  x = add_sat(x, __builtin_amdgcn_update_dpp(0, x, kRowBcast31, 0xc, 0xf, false));
-  if (lane == 63) wave_sum[wave] = x;
-  uint32_t before = __builtin_amdgcn_update_dpp(0, x, kWaveShr1, 0xf, 0xf, false);
+  const int wave = threadIdx.x >> 6;
+  const uint32_t upto = wave_scan(v, add_sat);
+  if ((threadIdx.x & 63) == 63) wave_sum[wave] = upto;
+  uint32_t before = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)upto, kWaveShr1, 0xf, 0xf, false);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   uint32_t sum = 0;
@@ -141,8 +134,8 @@ __global__ __launch_bounds__(256) void page_tables_kernel(PageTableArgs a) {
 // ---- rows into the pages and out of them -----------------------------------------------------------
 // Packed rows [T][heads][d] on one side, pages [pages][heads][page][d] on the other, both with free strides.  Bound by the memory: each
 // byte is read once and written once.  A workgroup takes a run of tokens: first one lane per token finds where the token lives (its
-// slot, or its sequence and table entry), then the lanes copy 16-byte chunks, one of K and one of V each.  (Small workgroups' worth of work, one
-// chunk a lane instead of four requested at once in runs four times as long: 655 MB gathered 252 -> 226 us, 41K tokens appended 73 -> 70.)
+// slot, or its sequence and table entry), then the lanes copy 16-byte chunks, one of K and one of V each.  (Four chunks
+// a lane, requested at once, in workgroups of eight times the tokens -> one: 655 MB gathered 252 -> 226 us, 41K tokens appended 73 -> 70.)
 //
 // Loads and stores through the caches or past them (bytes of K and V on one side; both sides are in the caches or not in turn as in a program
 // that goes on to other tensors): rows that are appended are not read soon, streaming stores 3000 to 60000 tokens, 8 heads of 128 (12 to
@@ -244,7 +237,8 @@ RowsArgs rows_args(const TensorView& k, const TensorView& v, const TensorView& k
   a.row_chunks = fast_div((uint32_t)k.heads << a.chunk_bits);
   // a chunk of K and of V to a thread, fewer tokens where the device would not be full
   const int most = std::min(std::max(kRowChunks / (int)a.row_chunks.d, 1), kMaxRowTokens);
-  a.tokens_per_group = std::max(1, std::min(most, ceil_div(a.T, 1024)));
+  // (and no more than 2^23 workgroups, 2^31 threads)
+  a.tokens_per_group = std::max({1, std::min(most, ceil_div(a.T, 1024)), ceil_div(a.T, 1 << 23)});
   return a;
 }
 int64_t rows_bytes(const TensorView& k) { return (int64_t)2 * k.L * k.heads * k.d * (k.dtype == BASA_BF16 ? 2 : 4); }

@@ -82,7 +82,7 @@ def test_decode(lib):  # noqa: F811
         assert call(**bad) == INVALID, bad
     assert call(q=query(d=96), kp=pages(d=96), vp=pages(d=96)) == UNSUPPORTED
     assert call(width=2 ** 27, stride=2 ** 27) == UNSUPPORTED
-    assert call(q=query(batch=2 ** 28)) == UNSUPPORTED
+    assert call(q=query(batch=2 ** 19 + 1)) == UNSUPPORTED and b"batch*heads" in lib.basa_last_error()
     assert call(q=query(batch=100), width=2 ** 26, stride=2 ** 26) == UNSUPPORTED and b"steps" in lib.basa_last_error()
     size = lambda q, kp, w: lib.basa_decode_workspace_size(C.byref(q), C.byref(kp), C.byref(kp), w)
     need = size(query(), pages(), 8)
