@@ -18,6 +18,11 @@
 //
 // The work is cut by tokens, not by sequences: paged_plan.hpp.  Every workgroup finds its run in the running sum of the lengths (they are
 // on the device), and the pieces that are not a whole sequence are joined by a second kernel.
+//
+// Measured (a pass that only reads: 7.05 TB/s): 64 sequences of 8000 to 60000 tokens, 32 heads on 8, d = 128, bf16, 7.6 GB: 1165 - 1190 us with
+// the join, 6.4 - 6.5 TB/s; half lines and ordinary loads 1435, whole lines 1330, whole lines and streaming loads 1190.  One sequence of 128K: 82 -
+// 86 + 4.8 us; f32, 16 heads of 64, 21 sequences of 3 to 5000: 34 + 4.2.  Level: the next tile's rows asked for before this one's products, 8
+// waves to a workgroup, fewer instructions in the exchange and in the rescaling.
 #include <algorithm>
 #include <climits>
 #include "common.hpp"
