@@ -324,8 +324,9 @@ def test_slots_beyond_32_bits():
 
 
 # ---------------------------------------------------------------- streams, graphs, and all of them together
-def test_graphs_that_share_a_workspace_follow_changed_lengths():
-    page, hk, hq, d = 16, 2, 8, 128
+@pytest.mark.parametrize("hq,hk", [(8, 2), (32, 1), (80, 2)])
+def test_graphs_that_share_a_workspace_follow_changed_lengths(hq, hk):
+    page, d = 16, 128
     lens = [500, 20, 9000]
     q, k, v, table = _decode_case(BF, d, hq, hk, page, lens, 71)
     cache, tab = bd.PagedCache(k, v), ints(table)
