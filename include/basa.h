@@ -346,9 +346,10 @@ basa_status basa_cache_gather(const basa_tensor* k_pages, const basa_tensor* v_p
  *   lse          out, nullable, [batch, heads_q] float.
  *   ws           workspace of basa_decode_workspace_size() bytes.  Nothing in it has to start at zero.
  * Tokens of a page that is none carry no weight, whatever the rows behind them hold; a query without any token gets a zero row and lse
- * = -inf, as does one whose scores are all -inf.  Accumulation, softmax state and partial results in fp32; with bf16 tensors the weights
- * enter the second product as the sum of two bf16 numbers.  Long sequences are split over workgroups: where goes by the lengths of the
- * whole call, so that a sequence agrees with itself called alone within rounding; repeating a call gives the same bits.
+ * = -inf, as does one whose scores are all -inf.  An infinite value makes its dimension infinite; NaN, two opposite infinities and one whose
+ * weight is zero (a score of -inf, an exponential below 2^-125) make it NaN.  Accumulation, softmax state and partial results in fp32; with
+ * bf16 tensors the weights enter the second product as the sum of two bf16 numbers.  Long sequences are split over workgroups: where goes
+ * by the lengths of the whole call, so that a sequence agrees with itself called alone within rounding; repeating a call gives the same bits.
  */
 size_t basa_decode_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t width);
 basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table,

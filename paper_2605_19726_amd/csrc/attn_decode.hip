@@ -14,7 +14,9 @@
 // tokens, chunk r of each row (whole rows, 16 lanes of 16 bytes), and turns its 8 x 8 block in registers, a byte permutation for two
 // numbers; output block e holds dimensions 8 r + e.  The running maximum is that of the lane's own column in every lane.
 // bf16: P goes in as the sum of two bf16 numbers (16 bits; the second product is free beside the loads), accumulation and softmax state in
-// fp32.  f32: the same on the fp32 matrix instruction, without the turning.
+// fp32.  The second number may be zero or negative, which times an infinite value is NaN where p v is infinite.  Nothing else can come of
+// that: a wave whose result holds NaN takes its tiles once more with two positive numbers for every positive p (2^-15 p at worst
+// in place of 2^-17 p), and the others pay one look at their result.  f32: the same on the fp32 matrix instruction, without the turning.
 //
 // The work is cut by tokens, not by sequences: paged_plan.hpp.  Every workgroup finds its run in the running sum of the lengths (they are
 // on the device), and the pieces that are not a whole sequence are joined by a second kernel.
@@ -82,6 +84,9 @@ __device__ __forceinline__ float weight_of(float s, float m, float scale_log2e) 
 __device__ __forceinline__ float lse_of(float m, float l, float scale) {
   return l == 0.f ? -INFINITY : fmaf(m, scale, __logf(l));
 }
+// p times this lies 3/4 to 3/2 steps of bf16 below p, so that its rounding is below p and the rest is positive, between 2^-10 p and 2^-6 p: a
+// bf16 number too down to p = 2^-125.
+constexpr float kBelow = 1.f - 0x3p-9f;
 // A cache that is read once: its lines are the first to leave the L2.  (Pays only where an instruction takes whole lines of 128 bytes: with half
 // lines, whose other half is asked for by the next instruction, they leave before that.)  Not where several units read the same rows.
 template <class T, bool kOnce>
@@ -210,13 +215,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       }
     floatx4 acc[kNT][kBlocks];
     float m[kNT], l[kNT];
-#pragma unroll
-    for (int nt = 0; nt < kNT; ++nt) {
-      m[nt] = -INFINITY;
-      l[nt] = 0.f;
-#pragma unroll
-      for (int e = 0; e < kBlocks; ++e) acc[nt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
-    }
     const int32_t* table = a.table + (int64_t)seq * a.table_stride;
     const char* k_head = a.k + kvh * a.k_h;
     const char* v_head = a.v + kvh * a.v_h;
@@ -233,138 +231,162 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       }
     };
     look_up(t0 + wave);
-    for (int t = t0 + wave; t < t1; t += kWaves) {
-      const bool valid = (unsigned)page_id < (unsigned)a.pages;
-      const uint32_t live = (uint32_t)__ballot(valid);
-      row_at[wave][lane >> 5][lane & 31] = valid ? page_id * page_stride + page_off * row_stride : 0;
-      look_up(t + kWaves);
-      uintx4 kf[2][kKSteps];
+#pragma clang loop unroll(disable)             // one copy: the first pass is not taken out of it
+    for (float first = 1.f;; first = kBelow) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+      for (int nt = 0; nt < kNT; ++nt) {
+        m[nt] = -INFINITY;
+        l[nt] = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {         // rows 8 i .. 8 i + 7 of the half, a line of 128 bytes each
-          const char* row = k_head + row_at[wave][0][16 * s + 8 * i + (r & 7)] + (r >> 3) * 64 + g * 16;
+        for (int e = 0; e < kBlocks; ++e) acc[nt][e] = floatx4{0.f, 0.f, 0.f, 0.f};
+      }
+      for (int t = t0 + wave; t < t1; t += kWaves) {
+        const bool valid = (unsigned)page_id < (unsigned)a.pages;
+        const uint32_t live = (uint32_t)__ballot(valid);
+        row_at[wave][lane >> 5][lane & 31] = valid ? page_id * page_stride + page_off * row_stride : 0;
+        look_up(t + kWaves);
+        uintx4 kf[2][kKSteps];
 #pragma unroll
-          for (int c = 0; c < kKSteps; c += 2) kf[s][c + i] = load_rows<uintx4, kOnce>(row + c * 64);
-        }
-      uint32_t vf[2][4][kVLoads][4];
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int s = 0; s < 2; ++s)
+          for (int i = 0; i < 2; ++i) {         // rows 8 i .. 8 i + 7 of the half, a line of 128 bytes each
+            const char* row = k_head + row_at[wave][0][16 * s + 8 * i + (r & 7)] + (r >> 3) * 64 + g * 16;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const char* row = v_head + row_at[wave][1][16 * s + 4 * g + j];
+            for (int c = 0; c < kKSteps; c += 2) kf[s][c + i] = load_rows<uintx4, kOnce>(row + c * 64);
+          }
+        uint32_t vf[2][4][kVLoads][4];
 #pragma unroll
-          for (int u = 0; u < kVLoads; ++u) {
-            if constexpr (kBf16 && kD == 64) {
-              const uintx2 w = load_rows<uintx2, kOnce>(row + r * 8);
-              vf[s][j][u][0] = w[0]; vf[s][j][u][1] = w[1];
-            } else {
-              const uintx4 w = load_rows<uintx4, kOnce>(row + r * 16 + u * 256);
+        for (int s = 0; s < 2; ++s)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) vf[s][j][u][e] = w[e];
+          for (int j = 0; j < 4; ++j) {
+            const char* row = v_head + row_at[wave][1][16 * s + 4 * g + j];
+#pragma unroll
+            for (int u = 0; u < kVLoads; ++u) {
+              if constexpr (kBf16 && kD == 64) {
+                const uintx2 w = load_rows<uintx2, kOnce>(row + r * 8);
+                vf[s][j][u][0] = w[0]; vf[s][j][u][1] = w[1];
+              } else {
+                const uintx4 w = load_rows<uintx4, kOnce>(row + r * 16 + u * 256);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vf[s][j][u][e] = w[e];
+              }
             }
           }
-        }
+        // Short rows, two waves: every load of a tile is requested before one is waited for, 1600 rows of 1 to 60 tokens 9.8 -> 9.2 us, 700 of 120 (40
+        // heads on 1) 26.3 -> 25.0.  More waves fill such gaps, and the compiler's order is better: one row of 700 10.1 -> 9.6, 16 of 1000 17.9 -> 16.5.
+        if constexpr (kBf16 && kWaves == 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int s = 0; s < 2; ++s)             // lanes r < 8 want both chunks of the first rows, the others both of the second
+        for (int s = 0; s < 2; ++s)             // lanes r < 8 want both chunks of the first rows, the others both of the second
 #pragma unroll
-        for (int c = 0; c < kKSteps; c += 2)
+          for (int c = 0; c < kKSteps; c += 2)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t x = kf[s][c][e], y = kf[s][c + 1][e], other = lane_xor<8>(r < 8 ? y : x);
-            kf[s][c][e] = r < 8 ? x : other;
-            kf[s][c + 1][e] = r < 8 ? other : y;
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t x = kf[s][c][e], y = kf[s][c + 1][e], other = lane_xor<8>(r < 8 ? y : x);
+              kf[s][c][e] = r < 8 ? x : other;
+              kf[s][c + 1][e] = r < 8 ? other : y;
+            }
+        floatx4 sc[kNT][2];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            if constexpr (kBf16) {
+              sc[nt][s] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int c = 0; c < kKSteps; ++c)
+                sc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[s][c]), __builtin_bit_cast(bf16x8, qf[nt][c]),
+                                                                    sc[nt][s], 0, 0, 0);
+            } else {                            // four sums of d / 4 products, then theirs: less than half the error of one sum of d
+              floatx4 x[4] = {};
+#pragma unroll
+              for (int c = 0; c < kKSteps; ++c)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  x[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[s][c][e]), __uint_as_float(qf[nt][c][e]), x[e], 0, 0, 0);
+              sc[nt][s] = (x[0] + x[1]) + (x[2] + x[3]);
+            }
           }
-      floatx4 sc[kNT][2];
+        if (live != 0xffffffffu) {              // past the end, or a page that is none: no weight, whatever the rows hold
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const bool on = (live >> (16 * s + 4 * g + j)) & 1;
+#pragma unroll
+              for (int nt = 0; nt < kNT; ++nt) sc[nt][s][j] = on ? sc[nt][s][j] : -INFINITY;
+#pragma unroll
+              for (int u = 0; u < kVLoads; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vf[s][j][u][e] = on ? vf[s][j][u][e] : 0u;
+            }
+        }
+        bf16x8 hi[kNT], lo[kNT];
+#pragma unroll
+        for (int nt = 0; nt < kNT; ++nt) {
+          float top = m[nt];
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[nt][s][j]);
+          top = column_max(top);
+          const float old = weight_of(m[nt], top, a.scale_log2e);
+          m[nt] = top;
+          float sum = 0.f;
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p = weight_of(sc[nt][s][j], top, a.scale_log2e);
+              sc[nt][s][j] = p;
+              sum += p;
+              if constexpr (kBf16) {
+                const __bf16 h = (__bf16)(p * first);
+                hi[nt][4 * s + j] = h;
+                lo[nt][4 * s + j] = (__bf16)(p - (float)h);
+              }
+            }
+          l[nt] = fmaf(l[nt], old, sum);
+#pragma unroll
+          for (int e = 0; e < kBlocks; ++e) acc[nt][e] *= old;
+        }
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int e = 0; e < kBlocks; ++e) {
+            // eight tokens of dimension kBlocks r + e
+            constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
+            uintx4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              w[j] = __builtin_amdgcn_perm(vf[j >> 1][2 * (j & 1) + 1][0][e >> 1], vf[j >> 1][2 * (j & 1)][0][e >> 1], e & 1 ? kHigh : kLow);
+#pragma unroll
+            for (int nt = 0; nt < kNT; ++nt) {
+              acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), hi[nt], acc[nt][e], 0, 0, 0);
+              acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), lo[nt], acc[nt][e], 0, 0, 0);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+              for (int e = 0; e < kBlocks; ++e)
+#pragma unroll
+                for (int nt = 0; nt < kNT; ++nt)
+                  acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[s][j][e >> 2][e & 3]), sc[nt][s][j], acc[nt][e], 0, 0, 0);
+        }
+      }
+      if (!kBf16 || first == kBelow) break;
+      float any = 0.f;                        // NaN if one of them is
 #pragma unroll
       for (int nt = 0; nt < kNT; ++nt)
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          if constexpr (kBf16) {
-            sc[nt][s] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
-            for (int c = 0; c < kKSteps; ++c)
-              sc[nt][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[s][c]), __builtin_bit_cast(bf16x8, qf[nt][c]),
-                                                                  sc[nt][s], 0, 0, 0);
-          } else {                            // four sums of d / 4 products, then theirs: less than half the error of one sum of d
-            floatx4 x[4] = {};
-#pragma unroll
-            for (int c = 0; c < kKSteps; ++c)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                x[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[s][c][e]), __uint_as_float(qf[nt][c][e]), x[e], 0, 0, 0);
-            sc[nt][s] = (x[0] + x[1]) + (x[2] + x[3]);
-          }
-        }
-      if (live != 0xffffffffu) {              // past the end, or a page that is none: no weight, whatever the rows hold
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const bool on = (live >> (16 * s + 4 * g + j)) & 1;
-#pragma unroll
-            for (int nt = 0; nt < kNT; ++nt) sc[nt][s][j] = on ? sc[nt][s][j] : -INFINITY;
-#pragma unroll
-            for (int u = 0; u < kVLoads; ++u)
-#pragma unroll
-              for (int e = 0; e < 4; ++e) vf[s][j][u][e] = on ? vf[s][j][u][e] : 0u;
-          }
-      }
-      bf16x8 hi[kNT], lo[kNT];
-#pragma unroll
-      for (int nt = 0; nt < kNT; ++nt) {
-        float top = m[nt];
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[nt][s][j]);
-        top = column_max(top);
-        const float old = weight_of(m[nt], top, a.scale_log2e);
-        m[nt] = top;
-        float sum = 0.f;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p = weight_of(sc[nt][s][j], top, a.scale_log2e);
-            sc[nt][s][j] = p;
-            sum += p;
-            if constexpr (kBf16) {
-              const __bf16 h = (__bf16)p;
-              hi[nt][4 * s + j] = h;
-              lo[nt][4 * s + j] = (__bf16)(p - (float)h);
-            }
-          }
-        l[nt] = fmaf(l[nt], old, sum);
-#pragma unroll
-        for (int e = 0; e < kBlocks; ++e) acc[nt][e] *= old;
-      }
-      if constexpr (kBf16) {
-#pragma unroll
-        for (int e = 0; e < kBlocks; ++e) {
-          // eight tokens of dimension kBlocks r + e
-          constexpr uint32_t kLow = 0x05040100, kHigh = 0x07060302;
-          uintx4 w;
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            w[j] = __builtin_amdgcn_perm(vf[j >> 1][2 * (j & 1) + 1][0][e >> 1], vf[j >> 1][2 * (j & 1)][0][e >> 1], e & 1 ? kHigh : kLow);
-#pragma unroll
-          for (int nt = 0; nt < kNT; ++nt) {
-            acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), hi[nt], acc[nt][e], 0, 0, 0);
-            acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), lo[nt], acc[nt][e], 0, 0, 0);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int e = 0; e < kBlocks; ++e)
-#pragma unroll
-              for (int nt = 0; nt < kNT; ++nt)
-                acc[nt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[s][j][e >> 2][e & 3]), sc[nt][s][j], acc[nt][e], 0, 0, 0);
-      }
+          for (int i = 0; i < 4; i += 2)
+            any = __builtin_elementwise_maximum(__builtin_elementwise_maximum(any, acc[nt][e][i]), acc[nt][e][i + 1]);
+      if (__ballot(any != any) == 0) break;
+      look_up(t0 + wave);
     }
 
     // the waves together.  Block e, register i of lane (g, n): head n; dimension kBlocks (4 g + i) + e (bf16), 64 (e / 4) + 4 (4 g + i) +
