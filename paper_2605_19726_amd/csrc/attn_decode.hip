@@ -94,6 +94,10 @@ __device__ __forceinline__ T load_rows(const char* at) {
   if constexpr (kOnce) return __builtin_nontemporal_load(reinterpret_cast<const T*>(at));
   return *reinterpret_cast<const T*>(at);
 }
+// Without any weight: zero, whatever the values are.
+__device__ __forceinline__ floatx4 normalised(floatx4 o, float sum) {
+  return sum == 0.f ? floatx4{0.f, 0.f, 0.f, 0.f} : o * (1.0f / sum);
+}
 template <bool kBf16>
 __device__ __forceinline__ void store4(char* at, floatx4 o) {
   if constexpr (kBf16) {
@@ -423,7 +427,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
         o += *reinterpret_cast<const floatx4*>(part + (w * a.part_heads + h) * kPitch + 4 * c) * f;
       }
       if (whole) {
-        store4<kBf16>(a.out + seq * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
+        store4<kBf16>(a.out + seq * a.out_b + (h0 + h) * a.out_h + c * 4 * kElem, normalised(o, sum));
         if (a.lse && c == 0) a.lse[(int64_t)seq * a.heads_kv * a.group + h0 + h] = lse_of(top, sum, a.scale);
       } else {
         const int64_t at = (int64_t)place * a.part_heads + h;
@@ -517,7 +521,7 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void decode_join_k
     sum = fmaf(row_ml[mine][i].y, f, sum);
     o += row_o[mine][i][c] * f;
   }
-  store4<kBf16>(a.out + b * a.out_b + head * a.out_h + c * 4 * kElem, o * (sum == 0.f ? 0.f : 1.0f / sum));
+  store4<kBf16>(a.out + b * a.out_b + head * a.out_h + c * 4 * kElem, normalised(o, sum));
   if (a.lse && c == 0) a.lse[id] = lse_of(top, sum, a.scale);
 }
 

@@ -74,3 +74,18 @@ def test_infinite_values_of_tiny_weight(dtype, d, width):
             v[int(table[i, t // 16]), :, t % 16, 11 + j] = INF if j % 3 else -INF
     out = bd.basa_decode_attn(q, bd.PagedCache(k, v), ints(table), ints(lens))
     _check(out, q, k, v, table, lens, [0, 1])
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("hq,hk,lens,width", PATHS)
+def test_a_row_of_scores_of_minus_infinity_is_zero_whatever_its_values(dtype, d, hq, hk, lens, width):
+    q, k, v, table = _decode_case(dtype, d, hq, hk, 16, lens, 23, width=width)
+    q[:, :, 0] = 1.0
+    for i in (0, 2):
+        at, off = (x.to(DEV) for x in rows_of(table[i], lens[i], 16))
+        k[at, :, off, 0] = -INF
+        v[at, :, off, :3] = torch.tensor([INF, -INF, NAN], dtype=dtype, device=DEV)
+    out, lse = bd.basa_decode_attn(q, bd.PagedCache(k, v), ints(table), ints(lens), want_lse=True)
+    for i in (0, 2):
+        assert not out[i].any() and (lse[i] == -INF).all()
+    _check(out, q, k, v, table, lens, [1, 3])
