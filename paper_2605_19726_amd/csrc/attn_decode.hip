@@ -511,11 +511,11 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void decode_join_k
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   if (row > 0 || !split) return;
-  float top = -INFINITY, sum = 0.f;
-#pragma unroll
+  float top = -INFINITY, sum = 0.f;           // (8 rows at a time: of d = 64 there are 64, more than there are registers for)
+#pragma unroll 8
   for (int i = 0; i < kRows; ++i) top = fmaxf(top, row_ml[mine][i].x);
   o = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
+#pragma unroll 8
   for (int i = 0; i < kRows; ++i) {
     const float f = weight_of(row_ml[mine][i].x, top, a.scale_log2e);
     sum = fmaf(row_ml[mine][i].y, f, sum);
