@@ -185,13 +185,19 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 # What torch.cuda.current_stream(device).cuda_stream and torch.cuda.current_device() give, without the Stream object (2 us a call) and the check
-# that the device is initialised (tensors on it are in hand).
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
+# that the device is initialised (tensors on it are in hand).  A torch that lacks the short ways takes the public ones.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _gpu_index(device) -> int:
+    if device.index is None:
+        raise ValueError(f"expected tensors on a GPU, got them on {device}")
+    return device.index
 
 
 def _stream(x: torch.Tensor):
-    return _raw_stream(x.device.index)
+    return _raw_stream(_gpu_index(x.device))
 
 
 def _ws(nbytes: int, device) -> torch.Tensor:
@@ -487,7 +493,7 @@ def _packed_desc(x: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
 
 def _launch(entry, device, *args):
     """A library call on the device's current stream, with that device as the current one (its launches go there)."""
-    index = device.index
+    index = _gpu_index(device)
     if index == _current_device():
         status = entry(*args, _raw_stream(index))
     else:
