@@ -122,17 +122,16 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
   __shared__ int64_t row_at[kWaves][2][kDecodeTile];         // K, V
   float2* const part_ml = reinterpret_cast<float2*>(part + kWaves * a.part_heads * kPitch);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, r = lane & 15;
-  const int per_seq = kSplit ? a.heads_kv : a.heads_kv * a.units;
+  const int per_seq = a.heads_kv;
 
-  // the run of this workgroup and the sequence that its first place is of: every wave finds them for itself
-  int b = 0, first = 0, run = 0, begin = 0, end = 1, group = 0, sub = 0;
+  // the run of this workgroup (or its sequence and head) and the sequence that its first place is of: every wave finds them for itself
+  int b = 0, first = 0, run = 0, begin = 0, end = 1, group = blockIdx.x, sub = 0;
+  if (a.units > 1) {                            // those of the units of one run: at the same time on one XCD, whose L2 has the rows then
+    const int line = blockIdx.x / (8 * a.units), rest = blockIdx.x - line * 8 * a.units;
+    group = line * 8 + (rest & 7);
+    sub = rest >> 3;
+  }
   if constexpr (kSplit) {
-    group = blockIdx.x;
-    if (a.units > 1) {                          // those of the units of one run: at the same time on one XCD, whose L2 has the rows then
-      const int line = blockIdx.x / (8 * a.units), rest = blockIdx.x - line * 8 * a.units;
-      group = line * 8 + (rest & 7);
-      sub = rest >> 3;
-    }
     if (a.batch <= kPlanBatch) {                // a few sequences to a lane
       const int each = (a.batch + 63) / 64;
       int places[kPlanBatch / 64], mine = 0;
@@ -176,7 +175,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       first = a.first_place[b];
     }
   } else {
-    b = blockIdx.x / per_seq;
+    if (group >= a.batch * per_seq) return;
+    b = group / per_seq;
   }
 
   for (int pos = begin; pos < end;) {
@@ -200,9 +200,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void decode_kernel(DecodeArgs a) {
       place = decode_part(piece, group) * a.units + sub;
       if (a.batch <= kPlanBatch && kvh == 0 && sub == 0 && t0 == 0 && tid == 0) a.first_place[seq] = seq_first;
     } else {
-      const int unit = blockIdx.x - b * per_seq;
-      kvh = unit / a.units;
-      sub = unit - kvh * a.units;
+      kvh = group - b * per_seq;
       pos = end;
     }
     const int h0 = kvh * a.group + sub * kHeads;
@@ -528,6 +526,8 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void decode_join_k
 // Query heads that share the loads of their KV head, a unit: up to 32 (bf16), 16 (f32, whose rows take twice the registers).  Of more heads there
 // are several units, whose workgroups read the rows at the same time through one L2: 64 sequences of 16384 tokens, 64 heads on 1, bf16 205 -> 148 us (each
 // unit by itself -> side by side, rows kept); 16 of 8192, 160 heads on 8, f32 373 -> 291; 320 heads 545 -> 377.
+// In one launch (streaming loads and neighbours in the grid -> side by side, rows kept): 500 of 700, 40 on 1, bf16 71 -> 59, 20 on 1, f32 130 -> 109; 64
+// of 700, 64 on 1, bf16 16.0 -> 14.0, f32 34 -> 24; 700 of 120, 40 on 1, bf16 25.2 -> 20.9; level: one of 300, 64 on 1.
 int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
 // One workgroup of 8 waves for all of a (sequence, run of query heads): no cut, no join, one launch.  A compute unit takes in some 64 GB/s, 2.2 us
 // for 256 tokens of bf16, d = 128, whatever its waves do; so that is for calls that are short, or have a workgroup for every compute unit and are
@@ -571,8 +571,16 @@ basa_status launch_kernel(const DecodeArgs& a, int groups, hipStream_t st) {
 template <bool kBf16, int kD, int kNT>
 basa_status launch(const DecodeArgs& a, int groups, hipStream_t st) {
   const int64_t units = (int64_t)a.batch * a.heads_kv * a.units;
-  if (is_solo(units, a.row_tokens) && has_small_workgroups(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 2, false>(a, (int)units, st);
-  if (is_solo(units, a.row_tokens)) return launch_kernel<kBf16, kD, kNT, 8, false>(a, (int)units, st);
+  if (is_solo(units, a.row_tokens)) {
+    const bool small = has_small_workgroups(units, a.row_tokens);
+    const int rows = a.batch * a.heads_kv;
+    if constexpr (!kBf16 || kNT > 1) {
+      const int groups = (int)align_up(rows, 8) * a.units;
+      if (a.units > 1) return small ? launch_kernel<kBf16, kD, kNT, 2, false, false>(a, groups, st)
+                                    : launch_kernel<kBf16, kD, kNT, 8, false, false>(a, groups, st);
+    }
+    return small ? launch_kernel<kBf16, kD, kNT, 2, false>(a, rows, st) : launch_kernel<kBf16, kD, kNT, 8, false>(a, rows, st);
+  }
   basa_status s = BASA_OK;
   if (a.batch > kPlanBatch) {
     ProfScope prof(K_DECODE, st);
