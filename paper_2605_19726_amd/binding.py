@@ -432,19 +432,27 @@ def _varlen_params(block, sparsity, beta: float = 1.0, sort: int = SORT_QK, wind
 # ---------------------------------------------------------------- paged key-value cache
 class PagedCache:
     """Keys and values in pages, indexed [pages, heads_kv, page, d]: the two tensors and their descriptors.  Any strides with a
-    contiguous d axis (a token-major store [pages, page, heads_kv, d] comes as its permute(0, 2, 1, 3))."""
+    contiguous d axis (a token-major store [pages, page, heads_kv, d] comes as its permute(0, 2, 1, 3)).  Other tensors make another
+    cache: what the descriptors were made from cannot be assigned."""
     __slots__ = ("k", "v", "device", "dtype", "pages", "heads", "page", "d", "_kd", "_vd")
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor):
-        self._kd, self._vd = tensor_desc(k), tensor_desc(v)
+        kd, vd = tensor_desc(k), tensor_desc(v)
         if k.shape != v.shape or k.dtype != v.dtype or k.device != v.device:
             raise ValueError("keys and values must agree in shape, dtype and device")
-        self.k, self.v, self.device, self.dtype = k, v, k.device, k.dtype
-        self.pages, self.heads, self.page, self.d = k.shape
-        for desc in (self._kd, self._vd):        # (the stride of an axis of one means nothing)
-            desc.stride_b = desc.stride_b if self.pages > 1 else 0
-            desc.stride_h = desc.stride_h if self.heads > 1 else 0
-            desc.stride_l = desc.stride_l if self.page > 1 else self.d
+        pages, heads, page, d = k.shape
+        for desc in (kd, vd):                    # (the stride of an axis of one means nothing)
+            desc.stride_b = desc.stride_b if pages > 1 else 0
+            desc.stride_h = desc.stride_h if heads > 1 else 0
+            desc.stride_l = desc.stride_l if page > 1 else d
+        for name, value in zip(self.__slots__, (k, v, k.device, k.dtype, pages, heads, page, d, kd, vd)):
+            object.__setattr__(self, name, value)
+
+    def __setattr__(self, name, value):
+        raise AttributeError(f"PagedCache.{name} cannot be assigned: make another cache")
+
+    def __reduce__(self):                        # a copy has descriptors of its own tensors
+        return PagedCache, (self.k, self.v)
 
 
 class PageTables:

@@ -1,0 +1,27 @@
+"""What the binding of the paged cache keeps from being misused (no GPU needed)."""
+import copy
+
+import pytest
+import torch
+
+from paper_2605_19726_amd import binding as bd
+
+
+def _cache(pages=9):
+    return bd.PagedCache(*(torch.zeros(pages, 4, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
+
+
+@pytest.mark.parametrize("name", ["k", "v", "device", "dtype", "pages", "heads", "page", "d"])
+def test_a_cache_cannot_come_apart_from_its_descriptors(name):
+    """Another tensor in the place of k or v would leave the kernels with the old one's address."""
+    cache, other = _cache(), _cache(12)
+    with pytest.raises(AttributeError):
+        setattr(cache, name, getattr(other, name))
+    assert cache.k.data_ptr() == cache._kd.ptr and cache.v.data_ptr() == cache._vd.ptr and cache.pages == 9
+
+
+def test_copies_of_a_cache_describe_their_own_tensors():
+    cache = _cache()
+    near, far = copy.copy(cache), copy.deepcopy(cache)
+    assert near.k is cache.k and near._kd.ptr == cache.k.data_ptr()
+    assert far.k.data_ptr() != cache.k.data_ptr() and far._kd.ptr == far.k.data_ptr() and far._vd.ptr == far.v.data_ptr()
