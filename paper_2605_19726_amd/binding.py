@@ -592,8 +592,8 @@ def basa_decode_attn(q, cache: PagedCache, table, lens, want_lse: bool = False, 
     if b:
         if ws is None:
             ws = _ws(lib.basa_decode_workspace_size(qd, cache._kd, cache._vd, width), dev)
-        elif ws.device != dev:
-            raise ValueError(f"ws must be on {dev}")
+        elif ws.device != dev or not ws.is_contiguous():         # (an expanded one has less memory than elements)
+            raise ValueError(f"ws must be a contiguous tensor on {dev}")
         sb, sh, _ = out.stride()
         ostr = _TwoStrides(sb if b > 1 else 0, sh if hq > 1 else d)
         _launch(lib.basa_decode_attn, dev, qd, cache._kd, cache._vd, tab, width, stride, at, out.data_ptr(), ostr, _ptr(lse), ws.data_ptr(), ws.numel())

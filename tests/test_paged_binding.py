@@ -25,3 +25,10 @@ def test_copies_of_a_cache_describe_their_own_tensors():
     near, far = copy.copy(cache), copy.deepcopy(cache)
     assert near.k is cache.k and near._kd.ptr == cache.k.data_ptr()
     assert far.k.data_ptr() != cache.k.data_ptr() and far._kd.ptr == far.k.data_ptr() and far._vd.ptr == far.v.data_ptr()
+
+
+def test_a_workspace_has_the_memory_that_its_size_says():
+    q, ints = torch.zeros(3, 8, 64, dtype=torch.bfloat16), lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    for ws in (torch.empty(1, dtype=torch.uint8).expand(1 << 20), torch.empty(1 << 21, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="ws must be"):
+            bd.basa_decode_attn(q, _cache(), ints(3, 7), ints(3), ws=ws)
