@@ -540,7 +540,7 @@ def basa_cache_append(k, v, slots, cache: PagedCache):
 
 def basa_cache_gather(cache: PagedCache, table, cu_seqlens, tokens: int, out=None):
     """(k, v), packed rows [tokens, heads_kv, d]: rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 (a device tensor) are the first tokens of sequence
-    i.  `out`: the two tensors to write into."""
+    i.  `out`: the two tensors to write into; rows before cu_seqlens[0] and from its last entry on keep what they hold (without `out`: anything)."""
     n = cu_seqlens.shape[0] - 1
     tab, width, stride = _block_table(table, n, cache.device)
     cu = _int_array(cu_seqlens, "cu_seqlens", cache.device, (n + 1,))
@@ -611,7 +611,8 @@ def ba_att_cached(q, k, v, cu_seqlens, cache: PagedCache, table, slots, cached=N
     """ba_att_varlen over a packed batch of prompts whose keys and values enter the cache: sequence i has rows cu_seqlens[i] ..
     cu_seqlens[i + 1] - 1 (host list) of q, k and v.  cached: host list of the tokens that a sequence held before; its new queries then meet
     all of them, read back from the pages, and the new ones (`causal` counts from the end: the last query sees every key).  Every sequence has to
-    have its slots: what basa_page_tables did not serve is not in the pages."""
+    have its slots: what basa_page_tables did not serve is not in the pages.  Rows of the result that belong to no sequence hold anything.  With
+    `cached` every sequence is a call of its own, and the offsets of the rows read back go to the device in a copy that waits: not for a graph."""
     cu = [int(t) for t in cu_seqlens]
     before = [0] * (len(cu) - 1) if cached is None else [int(t) for t in cached]
     if len(before) != len(cu) - 1 or any(t < 0 for t in before):

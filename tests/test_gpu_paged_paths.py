@@ -89,3 +89,32 @@ def test_copies_on_both_sides_of_the_streaming_lines(T, layout):
     gk, gv = bd.basa_cache_gather(cache, ints(table), ints([0, T - 100, T]), T)
     for got, rows, fill in ((gk, k, 7.0), (gv, v, 8.0)):
         assert torch.equal(bits(got[keep]), bits(rows[keep])) and (got[17] == fill).all()
+
+
+@pytest.mark.parametrize("cu", [[0, 90, 40], [50, 20, 90], [-5, 10, 30], [0, 2 ** 31 - 1, 2 ** 31 - 1], [-2 ** 31, 0, 60], [64, 0, 0], [3, 3, 61]])
+def test_gather_takes_rows_of_the_named_pages_alone_whatever_the_offsets(cu):
+    """Offsets that do not ascend, between guard rows and table entries that name other pages: rows outside [cu[0], cu[n]) stay as they were, every other
+    one is a row of a page that the table names, or zero."""
+    T, heads, page, d, pages, fill = 64, 2, 16, 64, 7, -3.0
+    place = torch.arange(5 * page, device=DEV).reshape(5, 1, page, 1).float()
+    caches = []
+    for first in (1.0, 101.0):              # K's rows hold 1 .. 80, V's 101 .. 180; pages 5 and 6, which no entry of the table names, 250
+        x = torch.full((pages, heads, page, d), 250.0, dtype=BF, device=DEV)
+        x[:5] = (place + first).to(BF)
+        caches.append(x)
+    around = torch.full((4, 7), 5, dtype=torch.int32, device=DEV)
+    around[3:], around[:, 5:] = 6, 6
+    around[1:3, 2:5] = torch.tensor([[3, 0, 4], [1, 2, 0]], dtype=torch.int32, device=DEV)
+    buffers = [torch.full((T + 40, heads, d), fill, dtype=BF, device=DEV) for _ in range(2)]
+    out = tuple(b[20:20 + T] for b in buffers)
+    bd.basa_cache_gather(bd.PagedCache(*caches), around[1:3, 2:5], ints(cu), T, out=out)
+    for buffer, first in zip(buffers, (1.0, 101.0)):
+        x = buffer.float()
+        assert (x[:20] == fill).all() and (x[20 + T:] == fill).all()
+        rows, inside = x[20:20 + T], torch.tensor([cu[0] <= t < cu[2] for t in range(T)], device=DEV)
+        assert (rows[~inside] == fill).all()
+        value = rows[inside][:, 0, 0]
+        assert (rows[inside] == value[:, None, None]).all()              # a row in one piece
+        assert ((value == 0) | ((value >= first) & (value < first + 5 * page))).all()
+    k, v = (b[20:20 + T, 0, 0].float() for b in buffers)
+    assert torch.equal(torch.where(k > 0, k + 100, k), v)                # K and V of the same place
