@@ -617,8 +617,11 @@ def ba_att_cached(q, k, v, cu_seqlens, cache: PagedCache, table, slots, cached=N
     before = [0] * (len(cu) - 1) if cached is None else [int(t) for t in cached]
     if len(before) != len(cu) - 1 or any(t < 0 for t in before):
         raise ValueError("cached: a length >= 0 for every sequence")
-    if cu[0] < 0 or any(a > b for a, b in zip(cu[:-1], cu[1:])) or cu[-1] > q.shape[0]:
-        raise ValueError(f"cu_seqlens must ascend within [0, {q.shape[0]}]")
+    rows = min(q.shape[0], k.shape[0])
+    if cu[0] < 0 or any(a > b for a, b in zip(cu[:-1], cu[1:])) or cu[-1] > rows:
+        raise ValueError(f"cu_seqlens must ascend within [0, {rows}]")
+    if any(before) and any(b > a and t + b - a > table.shape[1] * cache.page for t, a, b in zip(before, cu[:-1], cu[1:])):
+        raise ValueError(f"a table row has room for {table.shape[1] * cache.page} tokens, a sequence has more")
     basa_cache_append(k, v, slots, cache)
     if not any(before):
         return ba_att_varlen(q, k, v, cu, block, sparsity, **kw)
