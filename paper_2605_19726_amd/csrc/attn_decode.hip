@@ -21,10 +21,10 @@
 // The work is cut by tokens, not by sequences: paged_plan.hpp.  Every workgroup finds its run in the running sum of the lengths (they are
 // on the device), and the pieces that are not a whole sequence are joined by a second kernel.
 //
-// Measured (a pass that only reads: 7.05 TB/s): 64 sequences of 8000 to 60000 tokens, 32 heads on 8, d = 128, bf16, 7.6 GB: 1165 - 1190 us with
-// the join, 6.4 - 6.5 TB/s; half lines and ordinary loads 1435, whole lines 1330, whole lines and streaming loads 1190.  One sequence of 128K: 82 -
-// 86 + 4.8 us; f32, 16 heads of 64, 21 sequences of 3 to 5000: 34 + 4.2.  Level: the next tile's rows asked for before this one's products, 8
-// waves to a workgroup, fewer instructions in the exchange and in the rescaling.
+// Measured (a pass that only reads: 7.05 TB/s): 64 sequences of 8000 to 60000 tokens, 32 heads on 8, d = 128, bf16, 7.6 GB: 1170 us a call, with
+// the join, 6.5 TB/s (main kernel alone, when it was built: half lines and ordinary loads 1435, whole lines 1330, whole lines and streaming loads
+// 1190).  One sequence of 128K: 84 - 87 + 4.5 - 5.4 us; f32, 16 heads of 64, 21 sequences of 3 to 5000: 34 - 35 + 4.1 - 4.6.  Level: the next tile's
+// rows asked for before this one's products, 8 waves to a workgroup, fewer instructions in the exchange and in the rescaling.
 #include <algorithm>
 #include <climits>
 #include "common.hpp"
@@ -529,15 +529,17 @@ __global__ __launch_bounds__(kThreads > 256 ? kThreads : 256) void decode_join_k
 // In one launch (streaming loads and neighbours in the grid -> side by side, rows kept): 500 of 700, 40 on 1, bf16 71 -> 59, 20 on 1, f32 130 -> 109; 64
 // of 700, 64 on 1, bf16 16.0 -> 14.0, f32 34 -> 24; 700 of 120, 40 on 1, bf16 25.2 -> 20.9; level: one of 300, 64 on 1.
 int heads_per_unit(int group, bool bf16) { return bf16 && group > 16 ? 32 : 16; }
-// One workgroup of 8 waves for all of a (sequence, run of query heads): no cut, no join, one launch.  A compute unit takes in some 64 GB/s, 2.2 us
-// for 256 tokens of bf16, d = 128, whatever its waves do; so that is for calls that are short, or have a workgroup for every compute unit and are
-// not long.  One launch -> two (32 heads on 8, d = 128): one sequence of 256 tokens 6.1 -> 5.7 + 3.4 us on the device, of 700 10.6 -> 5.8 + 3.4, of
-// 1024 12.8 -> 5.7 + 3.4; from the host 10.3 -> 12.4 for all of them; 64 of 200 to 1000 31.7 -> 28.5 + 4.5, 16 of 1000 18.1 -> 16.0 + 4.1.
+// One workgroup of 8 waves for all of a (sequence, run of query heads): no cut, no join, one launch.  Every further 256 tokens, a tile for each wave,
+// take 1 to 3 us (bf16, d = 128; one sequence of 256, 512, 768, 1024: 7.0, 7.8, 10.8, 13.0 us); so that is for calls that are short, or have a workgroup
+// for every other compute unit and are not long.  One launch -> two (32 heads on 8, d = 128): one sequence of 256 tokens 7.0 -> 5.3 + 4.8 us on the device,
+// of 700 9.8 -> 5.8 + 4.2 - 5.3, of 1024 13.0 -> 6.0 + 5.3; calls one after the other 7.3 -> 9.6, 9.9 -> 10.1, 13.0 -> 10.4; 64 of 200 to 1000
+// 29.7 -> 28.4 + 4.1, 16 of 1000 16.2 - 17.6 -> 16.0 + 4.1.
 bool is_solo(int64_t units, int row_tokens) { return row_tokens <= 768 || (row_tokens <= 1024 && units >= kCUs / 2); }
 // Many short rows: workgroups of 2 waves, of which each compute unit holds more, so that the end of one overlaps others; a line between rows
-// that are long beside their number and the reverse.  8 waves -> 2: 1600 rows of 1 to 60 tokens 17.9 -> 8.7 us, 1600 of 60 to 120 23 -> 16, 1024 of
-// 20 to 500 24.8 -> 22.5, 8000 of 100 to 250 145 -> 114, 8000 of 100 to 1000 299 -> 277; level: 2048 of 100 to 1000 (80 / 81); kept at 8: 64 rows
-// of 100 to 250 6.7 / 9.4, 1024 of 20 to 1000 (d = 64) 20 / 24.
+// that are long beside their number and the reverse.  8 waves -> 2, 4 heads on 1, d = 128, lengths spread over their logarithm: 1600 rows of 1 to 60 tokens
+// 19.2 -> 7.6 us, 1600 of 60 to 120 24.5 -> 16.2, 1024 of 20 to 500 25.0 -> 24.1, 8000 of 100 to 250 151 -> 114, 8000 of 100 to 1000 283 -> 272, 2048 of 100 to
+// 1000 81 -> 85; kept at 8: 64 rows of 100 to 250 7.5 / 8.5, 1024 of 20 to 1000 (d = 64) 20 / 24.  Evenly spread: 20.5 -> 8.5, 25 -> 16.5, 30 -> 30.5, 156 ->
+// 121, 364 -> 370, 99 -> 106; 7.5 / 8.6, 27.4 / 29.5.
 bool has_small_workgroups(int64_t units, int row_tokens) { return units >= 2 * row_tokens; }
 int64_t most_places(int batch, int heads_kv, int group, bool bf16, int row_tokens) {
   return (int64_t)batch * heads_kv * ceil_div(group, heads_per_unit(group, bf16)) * decode_places(row_tokens);

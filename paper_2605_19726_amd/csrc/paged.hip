@@ -39,8 +39,9 @@ __device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t* all, uint32
 //
 // Bound by latency: a step of 600 sequences reads and writes some 100 KB.  One launch without a hand-over between workgroups: every
 // workgroup forms both running sums for itself (two words per sequence from the L2) and keeps them in the LDS, where its tokens look
-// their sequence up.  The token that opens a page writes the page's table entry.  8 sequences, 8 tokens: 3.0 us; 40 sequences, 85000 tokens
-// 5.0; 600 sequences, 15000 tokens 7.1; a kernel that does nothing 2.5.
+// their sequence up.  The token that opens a page writes the page's table entry.  8 sequences, 8 tokens: 2.8 us; 40 sequences, 85000 tokens
+// 5.3; 600 sequences, 15000 tokens 7.2; a step of 2000 sequences 9.0, of 8192 37, most of it the rounds of 256 lengths that are loaded one
+// after the other; a kernel that does nothing 2.5.
 struct PageTableArgs {
   const int32_t *have, *add, *free_pages;
   int32_t *table, *lens, *cu, *pages;

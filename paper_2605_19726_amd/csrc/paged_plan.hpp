@@ -36,11 +36,13 @@ constexpr int kDecodeTile = 32, kDecodeWaves = 4, kDecodeStep = kDecodeTile * kD
 constexpr int kDecodeLead = 1;
 BASA_HD int decode_steps(int len) { return len <= kDecodeStep ? 1 : (len + kDecodeStep - 1) / kDecodeStep; }
 BASA_HD int decode_places(int len) { return decode_steps(len) + kDecodeLead; }
-// The length of a run: two workgroups fit a compute unit, so short rows are cut into as many runs as there is room for at once.  Where
-// those would be longer than 24 steps there are more, down to 8 steps, so that a workgroup that is done early is followed by another; 2048
-// at most, which is as far as that helps.  Main kernel + join, one round -> runs of 8 and more: 1024 (sequence, head) of 2000 tokens, d = 128:
-// 205 + 4 -> 167 + 4 us; 2048 of 100 to 4000: 218 + 10.5 -> 185 + 11; one sequence of 128K tokens, 8 heads (17 steps): 86 + 5.8, in runs
-// of 8 89 + 9.3.
+// The length of a run: two workgroups fit a compute unit (bf16 d = 64: four, f32 d = 64: three), so short rows are cut into as many runs as there is
+// room for at once.  Where those would be longer than 24 steps there are more, down to 8 steps, so that a workgroup that is done early is
+// followed by another; 2048 at most.  That pays for long rows of pages stored token by token, and costs elsewhere.  Main kernel + join, one
+// round -> runs of 8 and more, (sequence, head) of d = 128 in bf16 unless said; token by token: 512 of 8000 to 60000 tokens 968 + 4.2 -> 943 + 5.5
+// us, 128 of 65536 713 + 4.1 -> 681 + 4.5, 512 of 3000 at d = 64 76 + 4.0 -> 70 + 4.2, 2048 of 3900 to 4000 617 + 5.0 -> 655 + 6.0, 1024 of 2000 163 + 4.0 ->
+// 179 + 4.6; head by head: 512 of 8000 to 60000 906 + 4.2 -> 926 + 5.5, 128 of 65536 660 + 4.1 -> 671 + 4.5, 1024 of 2000 161 + 4.0 -> 172 + 4.4, f32 512 of 3000
+// 238 + 4.1 -> 270 + 4.2; one sequence of 128K, 8 heads (17 steps, one round either way): 86.6 + 4.8, in runs of 8 88.7 + 5.8.
 constexpr int kDecodeOneRound = 512, kDecodeMost = 2048, kDecodeLongRun = 24, kDecodeShortRun = 8;
 BASA_HD int decode_run(int total) {          // total < 2^31 - kDecodeMost
   const int one = (total + kDecodeOneRound - 1) / kDecodeOneRound, many = (total + kDecodeMost - 1) / kDecodeMost;
