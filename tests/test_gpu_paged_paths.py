@@ -118,3 +118,20 @@ def test_gather_takes_rows_of_the_named_pages_alone_whatever_the_offsets(cu):
         assert ((value == 0) | ((value >= first) & (value < first + 5 * page))).all()
     k, v = (b[20:20 + T, 0, 0].float() for b in buffers)
     assert torch.equal(torch.where(k > 0, k + 100, k), v)                # K and V of the same place
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("width", [2, 70])
+def test_batches_of_more_than_65535_rows(dtype, width):
+    """70000 sequences that share eight pages, in small workgroups and cut by runs."""
+    n, hq, hk, d, page, pages = 70000, 4, 2, 64, 16, 8
+    rng = np.random.default_rng(width)
+    k, v, q = randn((pages, hk, page, d), 1, dtype), randn((pages, hk, page, d), 2, dtype), randn((n, hq, d), 3, dtype, 2.0)
+    table = rng.integers(0, pages, (n, width)).astype(np.int32)
+    lens = [int(x) for x in rng.integers(0, 2 * page + 1, n)]
+    lens[n - 1], lens[n // 2] = width * page, width * page - 7
+    out, lse, one = _attend(q, k, v, table, lens)
+    assert one == (width == 2) and torch.isfinite(out).all()
+    some = [0, 1, 32767, 32768, n // 2 - 1, n // 2, 65535, 65536, n - 2, n - 1]
+    check_decode(out[some], lse[some], q[some], k, v, table[some], [lens[i] for i in some])
+    assert torch.equal(torch.isfinite(lse), (ints(lens) > 0)[:, None].expand(n, hq))

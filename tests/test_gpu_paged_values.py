@@ -89,3 +89,35 @@ def test_a_row_of_scores_of_minus_infinity_is_zero_whatever_its_values(dtype, d,
     for i in (0, 2):
         assert not out[i].any() and (lse[i] == -INF).all()
     _check(out, q, k, v, table, lens, [1, 3])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("hq,hk,lens,width", PATHS)
+def test_captured_calls_follow_values_that_become_infinite_and_finite_again(dtype, hq, hk, lens, width):
+    q, k, v, table = _decode_case(dtype, 128, hq, hk, 16, lens, 29, width=width)
+    cache, tab, now = bd.PagedCache(k, v), ints(table), ints(lens)
+    ws, out = torch.empty(bd.decode_workspace_size(q, cache, tab), dtype=torch.uint8, device=DEV), torch.empty_like(q)
+    finite = bd.basa_decode_attn(q, cache, tab, now)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        bd.basa_decode_attn(q, cache, tab, now, ws=ws, out=out)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bd.basa_decode_attn(q, cache, tab, now, ws=ws, out=out)
+    kept = v.clone()
+    for x in (None, INF, NAN, None, -INF, None):
+        v.copy_(kept)
+        if x is not None:
+            v[int(table[1, 2]), :, 5, 9] = x                   # token 37 of sequence 1
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = bd.basa_decode_attn(q, cache, tab, now)
+        assert torch.equal(out.isnan(), eager.isnan()) and torch.equal(out.nan_to_num(nan=3.0), eager.nan_to_num(nan=3.0))
+        if x is None:
+            assert torch.equal(out, finite)
+        else:
+            assert not torch.isfinite(out[1, :, 9]).any() and torch.isfinite(out[1, :, :9]).all() and torch.equal(out[0], finite[0])
