@@ -356,6 +356,92 @@ basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, c
                              int32_t width, int64_t table_stride, const int32_t* lens, void* out, const int64_t* out_strides, float* lse,
                              void* ws, size_t ws_bytes, void* stream);
 
+/*
+ * ---- Several new tokens of every sequence: trees of drafted tokens, chains, mixed steps ----
+ *
+ * A step (basa_page_tables) in which sequence i gets n_i tokens, rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 of the packed batch.  They may be a tree: token r follows
+ * token parents[r] of its sequence's new ones, or the context.  They enter the pages in their order (basa_cache_append), attend to the context and their
+ * own ancestors (basa_tree_attn), and once some are accepted, the kept ones are moved together (basa_cache_compact) and the sequence is
+ * as long as that.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending.
+ */
+
+/*
+ * Who sees whom: bit j % 64 of word j / 64 of row cu_seqlens[i] + r is set iff new token j of sequence i is token r or an ancestor of it.
+ *   parents      [tokens] int32, numbers within the sequence; a token whose parent is negative, or not before it, follows the context.
+ *   masks        out [tokens, words] int64, rows mask_stride >= words entries apart; words <= 64.
+ *   depths       out, nullable, [tokens] int32: ancestors that a token has (its position is the context's length + that).
+ * New tokens from 64 * words on have no bit: their masks are zero, their depth is -1.  Rows of no sequence are left as they were.
+ */
+basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, int32_t n_seq, int32_t tokens, int64_t* masks, int32_t words,
+                            int64_t mask_stride, int32_t* depths, void* stream);
+/*
+ * Attention (Eq. 1) of the new tokens over the pages.  Sequence i holds lens[i] tokens, the new ones, the last n_i of them, included (once they were appended);
+ * a new token sees every one before the new ones, and of those the ones whose bit is set in its mask.  With n_i = 1 and its own bit that is
+ * basa_decode_attn.  Sequences of one and of many new tokens may be mixed; one without any is no work.
+ *   q            [1, heads_q, T, d], packed rows; T * heads_q up to 2^24.  Query head h reads KV head h / (heads_q / heads_kv).
+ *   width        entries of a table row that may be in use.
+ *   lens         [n_seq] int32; lengths below 0 count as 0, beyond width * page as that.  If it is less than n_i, the first of the new tokens
+ *                are in no page, and no one sees them.
+ *   masks        nullable, [T, words] int64, as of basa_tree_masks; any bits do, a token need not see itself.  New tokens without a bit (from 64 *
+ *                words on) are seen by no one.  NULL: chains, new token r sees new tokens 0 .. r.
+ *   out          [T, heads_q, d], dtype of q, 16-byte aligned; rows of no sequence are left as they were.  out_strides: nullable HOST array of 2,
+ *                strides of its token and head axes in elements (multiples of 16 bytes, head stride >= d).  Rows of out must not alias each other or an
+ *                input.
+ *   lse          out, nullable, [T, heads_q] float.
+ *   ws           workspace of basa_tree_workspace_size() bytes.  Nothing in it has to start at zero.
+ * Tokens that a query does not see, or whose page is none, carry no weight, whatever their rows hold; a query without any token gets a zero row and lse = -inf, as
+ * does one whose scores are all -inf.  Infinite values, accuracy and splitting as with basa_decode_attn; how rows are put together goes by T and n_seq too.
+ * Pages and tokens of a cache lie less than 2^36 bytes apart.
+ */
+size_t basa_tree_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t n_seq, int32_t width);
+basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                           int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
+                           int32_t words, int64_t mask_stride, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,
+                           void* stream);
+/*
+ * Kept tokens moved together, in place: token start[i] + keep[i][j] of sequence i to start[i] + j, for j < count[i].  Of a tree: start = the context's length, keep =
+ * the accepted path.  Of a long context: start = 0, keep = what is not dropped.
+ *   start, count [n_seq] int32; counts beyond `most` count as that.
+ *   keep         [n_seq, most] int32, rows keep_stride >= most entries apart; the first count[i] of a row ascend strictly from 0 or more on.  (Of other lists it is
+ *                not defined which rows are moved; an entry below its own place, a place without a page or beyond the table row moves nothing.)
+ * The pages that are written to must belong to their sequence alone.  What stood behind the kept tokens stays there.
+ */
+basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
+                               const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,
+                               void* stream);
+/*
+ * Sequences that go on from others (samples of one prompt, the beams of a search): new sequence j is sequence parents[j] of the old table.  They share its whole
+ * pages; its page that is not full, if there is one, goes to the first of them, and each further one gets a page of its own, in order of j from the start of
+ * free_pages, and an entry in `copies`.  An old sequence that is no one's parent ends there (basa_page_free finds its pages).  A new
+ * sequence whose parent is none (outside [0, n_seq)) is empty, and so is one that is not served because free pages ran short.
+ *   table, lens  of the n_seq <= 8192 old sequences.  parents [n_new] int32, n_new <= 8192.
+ *   free_pages   [n_free] int32: pages that belong to no one, each once.
+ *   new_table    out, [n_new, width], rows new_stride apart: entries of pages in use are written, the others left as they were.
+ *   new_lens     out [n_new] int32.
+ *   copies       out [n_new, 3] int32, for basa_cache_copy on every cache of this table: page to copy from, page to copy to, tokens in it; -1, -1, 0 for none.
+ *   pages        out [2] int32: how many of free_pages were given out (the first ones), and how many would have been if none were short.
+ * No output may overlap an input or another output.
+ */
+basa_status basa_page_fork(const int32_t* table, int32_t width, int64_t table_stride, const int32_t* lens, int32_t n_seq, int32_t page,
+                           const int32_t* parents, int32_t n_new, const int32_t* free_pages, int32_t n_free, int32_t* new_table,
+                           int64_t new_stride, int32_t* new_lens, int32_t* copies, int32_t* pages, void* stream);
+/*
+ * Copies of pages: for every entry (from, to, tokens) of copies, DEVICE int32 [n, 3], the first `tokens` tokens of page `from` to page `to`, in K and V.  An
+ * entry one of whose pages is none is no copy; tokens beyond a page count as that.  No page may be copied to twice, or both to and from, in a call.
+ */
+basa_status basa_cache_copy(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* copies, int32_t n, void* stream);
+/*
+ * The pages that no sequence holds: those of 0 .. n_pages - 1 that are not among the first ceil(lens[i] / page) entries of any row, ascending.  A page that several hold is
+ * free when the last of them ends; a sequence that ends, or is cut back, gets its new length and nothing else.  (Whatever else has to be
+ * kept has a row: a prefix that stays for later prompts, say.)
+ *   free_pages   out [n_pages] int32: the free ones come first, the rest is left as it was.   count: out [1] int32, how many.
+ *   ws           workspace of basa_page_free_workspace_size() bytes.  Nothing in it has to start at zero.
+ * No output may overlap an input or another output.
+ */
+size_t basa_page_free_workspace_size(int32_t n_seq, int32_t width, int32_t n_pages);
+basa_status basa_page_free(const int32_t* table, int32_t width, int64_t table_stride, const int32_t* lens, int32_t n_seq, int32_t page,
+                           int32_t n_pages, int32_t* free_pages, int32_t* count, void* ws, size_t ws_bytes, void* stream);
+
 /* Reason of the last non-OK status returned on this thread (host string, owned by the
  * library, valid until the next failing call on the thread). */
 const char* basa_last_error(void);

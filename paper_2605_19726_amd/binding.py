@@ -30,6 +30,8 @@ EXPORTS = (
     "basa_block_radius", "basa_deviation_bound", "basa_selection_fidelity", "basa_pearson_sums",
     "basa_attn_best_workspace_size", "basa_varlen_workspace_size", "basa_varlen_attn", "basa_static_scratch_size", "basa_static_init", "basa_norm_sort_static",
     "basa_page_tables", "basa_cache_append", "basa_cache_gather", "basa_decode_workspace_size", "basa_decode_attn",
+    "basa_tree_masks", "basa_tree_workspace_size", "basa_tree_attn", "basa_cache_compact", "basa_page_fork", "basa_cache_copy",
+    "basa_page_free_workspace_size", "basa_page_free",
 )
 
 
@@ -134,6 +136,22 @@ def load():
     lib.basa_decode_workspace_size.argtypes = [T, T, T, C.c_int32]
     lib.basa_decode_attn.restype = C.c_int
     lib.basa_decode_attn.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, S3, V, V, C.c_size_t, V]
+    lib.basa_tree_masks.restype = C.c_int
+    lib.basa_tree_masks.argtypes = [V, V, C.c_int32, C.c_int32, V, C.c_int32, C.c_int64, V, V]
+    lib.basa_tree_workspace_size.restype = C.c_size_t
+    lib.basa_tree_workspace_size.argtypes = [T, T, T, C.c_int32, C.c_int32]
+    lib.basa_tree_attn.restype = C.c_int
+    lib.basa_tree_attn.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, V, C.c_int32, C.c_int64, V, S3, V, V, C.c_size_t, V]
+    lib.basa_cache_compact.restype = C.c_int
+    lib.basa_cache_compact.argtypes = [T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, C.c_int64, V, C.c_int32, V]
+    lib.basa_page_fork.restype = C.c_int
+    lib.basa_page_fork.argtypes = [V, C.c_int32, C.c_int64, V, C.c_int32, C.c_int32, V, C.c_int32, V, C.c_int32, V, C.c_int64, V, V, V, V]
+    lib.basa_cache_copy.restype = C.c_int
+    lib.basa_cache_copy.argtypes = [T, T, V, C.c_int32, V]
+    lib.basa_page_free_workspace_size.restype = C.c_size_t
+    lib.basa_page_free_workspace_size.argtypes = [C.c_int32, C.c_int32, C.c_int32]
+    lib.basa_page_free.restype = C.c_int
+    lib.basa_page_free.argtypes = [V, C.c_int32, C.c_int64, V, C.c_int32, C.c_int32, C.c_int32, V, V, V, C.c_size_t, V]
     lib.basa_calibrate_read.restype = C.c_int
     lib.basa_calibrate_read.argtypes = [V, C.c_size_t, V, V]
     lib.basa_calibrate_mfma.restype = C.c_int
@@ -637,6 +655,150 @@ def ba_att_cached(q, k, v, cu_seqlens, cache: PagedCache, table, slots, cached=N
             e0, e1 = ends[i], ends[i + 1]
             ba_att(view(q, a, b), view(ck, e0, e1), view(cv, e0, e1), block, sparsity, out=view(out, a, b), **kw)
     return out
+
+
+# ---------------------------------------------------------------- several new tokens of every sequence, and the pages around them
+def _int_rows(t: torch.Tensor, name: str, device, rows: int, dtype=torch.int32):
+    """(pointer, width, row stride) of a device array of integers [rows, width] with contiguous rows."""
+    if t.dim() != 2 or t.dtype != dtype or t.device != device or t.shape[0] != rows or \
+            (t.numel() > 1 and t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be a {dtype} tensor [{rows}, width] on {device} with contiguous rows")
+    width = t.shape[1]
+    return t.data_ptr(), width, t.stride(0) if rows > 1 else max(width, t.stride(0))
+
+
+def basa_tree_masks(parents, cu_seqlens, words: int, out=None):
+    """(masks [T, words] int64, depths [T] int32) of the drafted tokens of a step: bit j of a token's row is set iff it is drafted token j of its sequence or
+    follows it.  parents [T]: the drafted token of the same sequence that a token follows, -1 for the context.  cu_seqlens: a device tensor (PageTables.cu).
+    `out`: the two tensors to write into; rows of no sequence keep what they hold (without `out`: anything)."""
+    dev, T, n = parents.device, parents.shape[0], cu_seqlens.shape[0] - 1
+    if out is None:
+        masks, depths = torch.empty(T, int(words), dtype=torch.int64, device=dev), torch.empty(T, dtype=torch.int32, device=dev)
+    else:
+        masks, depths = out
+    at, width, stride = _int_rows(masks, "masks", dev, T, torch.int64)
+    if width != words:
+        raise ValueError(f"out: masks of {words} words")
+    _launch(load().basa_tree_masks, dev, _int_array(parents, "parents", dev, (T,)), _int_array(cu_seqlens, "cu_seqlens", dev, (n + 1,)), n, T,
+            at, width, stride, _int_array(depths, "depths", dev, (T,)))
+    return masks, depths
+
+
+def _new_rows_desc(q: torch.Tensor, name: str, cache: PagedCache) -> BasaTensor:
+    """Descriptor of packed query rows [T, heads_q, d]."""
+    shape = q.shape
+    if len(shape) != 3 or q.dtype != cache.dtype or q.device != cache.device or q.stride(2) != 1:
+        raise ValueError(f"{name} must be a {cache.dtype} tensor [tokens, heads, d] on {cache.device} with a contiguous d axis")
+    (T, h, d), (st, sh, _) = shape, q.stride()
+    return BasaTensor(q.data_ptr(), cache._kd.dtype, 1, h, T, d, 0, sh if h > 1 else 0, st if T > 1 else max(d, st))
+
+
+def tree_workspace_size(q, cache: PagedCache, table) -> int:
+    """Bytes of workspace for basa_tree_attn with tables of this shape."""
+    return int(load().basa_tree_workspace_size(_new_rows_desc(q, "q", cache), cache._kd, cache._vd, table.shape[0], table.shape[1]))
+
+
+def basa_tree_attn(q, cache: PagedCache, table, lens, cu_seqlens, masks=None, want_lse: bool = False, ws=None, out=None):
+    """Attention of the new tokens of every sequence, packed rows q [T, heads_q, d], sequence i's at cu_seqlens[i] .. cu_seqlens[i + 1] - 1 (a device tensor): each sees
+    the first lens[i] tokens of its pages but for the last ones, which are the new tokens themselves (appended before), and of those the ones in its row of `masks`
+    [T, words] (basa_tree_masks).  Without masks new token r sees new tokens 0 .. r.  Rows of `out` of no sequence keep what they hold (without `out`: anything).
+    The launch is sized by the table's width: table[:, :w] with the columns in use is faster than one with room for the longest context there is."""
+    lib, dev, n = load(), cache.device, cu_seqlens.shape[0] - 1
+    qd = _new_rows_desc(q, "q", cache)
+    T, hq, d = q.shape
+    tab, width, stride = _block_table(table, n, dev)
+    at, cu = _int_array(lens, "lens", dev, (n,)), _int_array(cu_seqlens, "cu_seqlens", dev, (n + 1,))
+    seen, words, mask_stride = (None, 0, 0) if masks is None else _int_rows(masks, "masks", dev, T, torch.int64)
+    if out is None:
+        out = torch.empty(T, hq, d, dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or out.stride(2) != 1:
+        raise ValueError("out must have the shape, dtype and device of q and a contiguous d axis")
+    lse = torch.empty(T, hq, dtype=torch.float32, device=dev) if want_lse else None
+    if T and n:
+        if ws is None:
+            ws = _ws(lib.basa_tree_workspace_size(qd, cache._kd, cache._vd, n, width), dev)
+        elif ws.device != dev or not ws.is_contiguous():
+            raise ValueError(f"ws must be a contiguous tensor on {dev}")
+        st, sh, _ = out.stride()
+        ostr = _TwoStrides(st if T > 1 else 0, sh if hq > 1 else d)
+        _launch(lib.basa_tree_attn, dev, qd, cache._kd, cache._vd, tab, width, stride, at, cu, n, seen, words, mask_stride, out.data_ptr(), ostr,
+                _ptr(lse), ws.data_ptr(), ws.numel())
+    return (out, lse) if want_lse else out
+
+
+def ba_att_tree(q, k, v, cache: PagedCache, table, lens, slots, cu_seqlens, masks=None, want_lse: bool = False, ws=None, out=None):
+    """One layer of a step with several new tokens per sequence, packed rows q [T, heads_q, d] and k, v [T, heads_kv, d]: they enter the cache at their slots and
+    attend to what their sequence holds.  table, lens, slots, cu_seqlens: of basa_page_tables, masks: of basa_tree_masks, once for all layers."""
+    basa_cache_append(k, v, slots, cache)
+    return basa_tree_attn(q, cache, table, lens, cu_seqlens, masks, want_lse, ws, out)
+
+
+def basa_cache_compact(cache: PagedCache, table, start, keep, count):
+    """Kept tokens of every sequence moved together, in place: token start[i] + keep[i, j] to start[i] + j, for j < count[i].  keep [n_seq, most]: ascending rows."""
+    dev, n = cache.device, start.shape[0]
+    tab, width, stride = _block_table(table, n, dev)
+    rows, most, keep_stride = _int_rows(keep, "keep", dev, n)
+    _launch(load().basa_cache_compact, dev, cache._kd, cache._vd, tab, width, stride, _int_array(start, "start", dev, (n,)), rows, most, keep_stride,
+            _int_array(count, "count", dev, (n,)), n)
+
+
+class PageFork:
+    """Outputs of basa_page_fork (device tensors) for n_new sequences with tables of `width` entries."""
+    __slots__ = ("_n", "_width", "_device", "_outs", "_ptrs")
+
+    def __init__(self, n_new: int, width: int, device):
+        ints = [torch.empty(shape, dtype=torch.int32, device=torch.device(device)) for shape in ((n_new, width), (n_new,), (n_new, 3), (2,))]
+        self._n, self._width, self._device, self._outs = n_new, width, ints[0].device, tuple(ints)
+        self._ptrs = tuple(t.data_ptr() for t in ints)
+
+    table = property(lambda self: self._outs[0], doc="[n_new, width] int32: block tables; entries that are not in use hold anything")
+    lens = property(lambda self: self._outs[1], doc="[n_new] int32: tokens that a sequence holds")
+    copies = property(lambda self: self._outs[2], doc="[n_new, 3] int32, for basa_cache_copy on every layer's cache: from, to, tokens; -1, -1, 0 for none")
+    pages = property(lambda self: self._outs[3], doc="[2] int32: free pages given out, and asked for")
+
+
+def basa_page_fork(table, lens, parents, free_pages, page: int, out: Optional[PageFork] = None) -> PageFork:
+    """Block tables of sequences that go on from others: new sequence j is old sequence parents[j].  Whole pages are shared; the copies of pages that are not full
+    are made by basa_cache_copy."""
+    dev, n, m = table.device, lens.shape[0], parents.shape[0]
+    tab, width, stride = _block_table(table, n, dev)
+    if out is None:
+        out = PageFork(m, width, dev)
+    elif out._n != m or out._width != width or out._device != dev:
+        raise ValueError(f"out: a PageFork({m}, {width}, {dev})")
+    new_table, new_lens, copies, pages = out._ptrs
+    _launch(load().basa_page_fork, dev, tab, width, stride, _int_array(lens, "lens", dev, (n,)), n, int(page), _int_array(parents, "parents", dev, (m,)), m,
+            _int_array(free_pages, "free_pages", dev, free_pages.shape[:1]), free_pages.shape[0], new_table, width, new_lens, copies, pages)
+    return out
+
+
+def basa_cache_copy(cache: PagedCache, copies):
+    """Copies of pages, K and V: the first copies[i, 2] tokens of page copies[i, 0] to page copies[i, 1]; entries that name no page are left out."""
+    n = copies.shape[0]
+    _launch(load().basa_cache_copy, cache.device, cache._kd, cache._vd, _int_array(copies, "copies", cache.device, (n, 3)), n)
+
+
+def page_free_workspace_size(table, pages: int) -> int:
+    """Bytes of workspace for basa_page_free with a table of this shape and a cache of so many pages."""
+    return int(load().basa_page_free_workspace_size(table.shape[0], table.shape[1], int(pages)))
+
+
+def basa_page_free(table, lens, page: int, pages: int, out=None, ws=None):
+    """(free_pages [pages] int32, count [1] int32): the first count entries are the pages that no sequence holds, ascending; the others keep what they hold (without
+    `out`: anything)."""
+    lib, dev, n = load(), table.device, lens.shape[0]
+    tab, width, stride = _block_table(table, n, dev)
+    if out is None:
+        free, count = (torch.empty(size, dtype=torch.int32, device=dev) for size in (int(pages), 1))
+    else:
+        free, count = out
+    if ws is None:
+        ws = _ws(lib.basa_page_free_workspace_size(n, width, int(pages)), dev)
+    elif ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous tensor on {dev}")
+    _launch(lib.basa_page_free, dev, tab, width, stride, _int_array(lens, "lens", dev, (n,)), n, int(page), int(pages),
+            _int_array(free, "free_pages", dev, (int(pages),)), _int_array(count, "count", dev, (1,)), ws.data_ptr(), ws.numel())
+    return free, count
 
 
 def basa_profile_enable(on: bool):

@@ -36,7 +36,7 @@ const char* const kKernelNames[K_COUNT] = {
     "norm_tile_sort_kernel", "merge_pass_kernel", "block_stats_kernel",
     "block_scores_kernel", "row_select_kernel", "gather_kernels", "attn_mfma_kernel",
     "attn_f32_kernel", "block_mass_kernel", "diagnostic_small_kernels", "scores_select_kernel", "attn_combine_kernel",
-    "paged_cache_kernels", "decode_kernel", "decode_join_kernel"};
+    "paged_cache_kernels", "decode_kernel", "decode_join_kernel", "tree_kernel", "tree_join_kernel"};
 }  // namespace
 
 ProfScope::ProfScope(int id, hipStream_t st) : slot_(-1), st_(st) {
@@ -352,7 +352,7 @@ basa_status check_varlen(const basa_tensor* q, const basa_tensor* k, const basa_
 
 // ---- paged key-value cache ------------------------------------------------------------------
 // Largest counts that the kernels take as 32-bit numbers with room for a step beyond them.
-constexpr int kMaxPagedTokens = 1 << 30, kMaxDecodeRows = 1 << 22;
+constexpr int kMaxPagedTokens = 1 << 30, kMaxDecodeRows = 1 << 22, kMaxTreeRows = 1 << 24;
 
 basa_status check_pages(const basa_tensor* k, const basa_tensor* v) {
   basa_status s;
@@ -417,6 +417,42 @@ basa_status check_decode(const basa_tensor* q, const basa_tensor* k, const basa_
   }
   return BASA_OK;
 }
+
+basa_status check_tree(const basa_tensor* q, const basa_tensor* k, const basa_tensor* v, int32_t n_seq, int32_t width) {
+  basa_status s;
+  if ((s = check_rows(q, "q")) != BASA_OK) return s;
+  if ((s = check_pages(k, v)) != BASA_OK) return s;
+  if (q->batch != 1) { set_error("q: packed rows (batch 1), got batch = %d", q->batch); return BASA_ERR_INVALID_ARG; }
+  if (q->dtype != k->dtype || q->d != k->d) { set_error("q and the pages must agree in dtype and head dimension"); return BASA_ERR_INVALID_ARG; }
+  if (q->heads % k->heads != 0) {
+    set_error("query heads (%d) must be a multiple of kv heads (%d)", q->heads, k->heads); return BASA_ERR_INVALID_ARG;
+  }
+  if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
+  if ((int64_t)q->L * q->heads > kMaxTreeRows) { set_error("q: tokens*heads exceeds %d", kMaxTreeRows); return BASA_ERR_UNSUPPORTED; }
+  const int64_t most = (int64_t)1 << 36, e = q->dtype == BASA_BF16 ? 2 : 4;
+  for (const basa_tensor* t : {k, v})
+    if (t->stride_b * e >= most || t->stride_l * e >= most) {
+      set_error("pages or tokens of a cache lie %lld bytes apart or more", (long long)most); return BASA_ERR_UNSUPPORTED;
+    }
+  if ((s = check_width(width, k->L)) != BASA_OK) return s;
+  if (!tree_takes(q->L, n_seq, q->heads, k->heads, q->d, q->dtype == BASA_BF16, width * k->L)) {
+    set_error("%d new tokens of %d sequences with room for %lld tokens each: more steps than a call takes", q->L, n_seq, (long long)width * k->L);
+    return BASA_ERR_UNSUPPORTED;
+  }
+  return BASA_OK;
+}
+// None of the outputs may overlap an input (what one workgroup reads, another may have written), or another output.
+struct Span { const void* at; size_t bytes; const char* name; };
+basa_status check_apart(const Span* in, size_t n_in, const Span* out, size_t n_out) {
+  for (size_t o = 0; o < n_out; ++o) {
+    for (size_t i = 0; i < n_in; ++i)
+      if (overlap(out[o].at, out[o].bytes, in[i].at, in[i].bytes)) { set_error("%s must not overlap %s", out[o].name, in[i].name); return BASA_ERR_INVALID_ARG; }
+    for (size_t p = 0; p < o; ++p)
+      if (overlap(out[o].at, out[o].bytes, out[p].at, out[p].bytes)) { set_error("%s must not overlap %s", out[o].name, out[p].name); return BASA_ERR_INVALID_ARG; }
+  }
+  return BASA_OK;
+}
+size_t rows_span(int32_t n, int64_t stride, int32_t width, size_t e) { return n > 0 ? ((size_t)(n - 1) * stride + width) * e : 0; }
 
 }  // namespace
 }  // namespace basa
@@ -764,18 +800,10 @@ basa_status basa_page_tables(const int32_t* have, const int32_t* add, int32_t n_
   if (n_free < 0 || (n_free > 0 && !free_pages)) { set_error("null free_pages, or a negative number of them (%d)", n_free); return BASA_ERR_INVALID_ARG; }
   if (n_slots < 0 || (n_slots > 0 && !slots)) { set_error("null slots, or a negative number of them (%d)", n_slots); return BASA_ERR_INVALID_ARG; }
   if (n_slots > kMaxPagedTokens) { set_error("more than %d slots in a call", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
-  // every workgroup reads all lengths: none of them may be written meanwhile
-  struct Span { const void* at; size_t bytes; const char* name; };
-  const size_t table_bytes = n_seq > 0 ? ((size_t)(n_seq - 1) * table_stride + width) * 4 : 0;
   const Span in[] = {{have, (size_t)n_seq * 4, "have"}, {add, (size_t)n_seq * 4, "add"}, {free_pages, (size_t)n_free * 4, "free_pages"}};
   const Span out[] = {{lens, (size_t)n_seq * 4, "lens"}, {cu_add, ((size_t)n_seq + 1) * 4, "cu_add"}, {pages, 8, "pages"},
-                      {slots, (size_t)n_slots * 8, "slots"}, {table, table_bytes, "table"}};
-  for (const Span& o : out) {
-    for (const Span& i : in)
-      if (overlap(o.at, o.bytes, i.at, i.bytes)) { set_error("%s must not overlap %s", o.name, i.name); return BASA_ERR_INVALID_ARG; }
-    for (const Span* p = out; p != &o; ++p)
-      if (overlap(o.at, o.bytes, p->at, p->bytes)) { set_error("%s must not overlap %s", o.name, p->name); return BASA_ERR_INVALID_ARG; }
-  }
+                      {slots, (size_t)n_slots * 8, "slots"}, {table, rows_span(n_seq, table_stride, width, 4), "table"}};
+  if ((s = check_apart(in, 3, out, 5)) != BASA_OK) return s;
   return launch_page_tables(have, add, n_seq, page, table, width, table_stride, free_pages, n_free, slots, n_slots, lens, cu_add, pages,
                             reinterpret_cast<hipStream_t>(stream));
 }
@@ -830,6 +858,138 @@ basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, c
   if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
   return launch_decode_attn(view_of(*q), view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, out, out_b, out_h, lse, ws,
                             reinterpret_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"
+
+// ---- several new tokens of every sequence, and the pages around them --------------------------------
+extern "C" {
+
+basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, int32_t n_seq, int32_t tokens, int64_t* masks, int32_t words,
+                            int64_t mask_stride, int32_t* depths, void* stream) {
+  if (n_seq < 0 || tokens < 0) { set_error("negative number of sequences (%d) or tokens (%d)", n_seq, tokens); return BASA_ERR_INVALID_ARG; }
+  if (tokens > kMaxPagedTokens) { set_error("more than %d tokens in a call", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
+  if (words < 1) { set_error("masks need words >= 1 (got %d)", words); return BASA_ERR_INVALID_ARG; }
+  if (words > kMaxMaskWords) { set_error("more than %d words to a mask (%d)", kMaxMaskWords, words); return BASA_ERR_UNSUPPORTED; }
+  if (mask_stride < words) { set_error("rows of masks are %lld words apart, %d wide", (long long)mask_stride, words); return BASA_ERR_INVALID_ARG; }
+  if (!cu_seqlens) { set_error("null cu_seqlens"); return BASA_ERR_INVALID_ARG; }
+  if (tokens > 0 && (!parents || !masks)) { set_error("null parents or masks"); return BASA_ERR_INVALID_ARG; }
+  if (reinterpret_cast<uintptr_t>(masks) % 8) { set_error("masks must be 8-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  const Span in[] = {{parents, (size_t)tokens * 4, "parents"}, {cu_seqlens, ((size_t)n_seq + 1) * 4, "cu_seqlens"}};
+  const Span out[] = {{masks, rows_span(tokens, mask_stride, words, 8), "masks"}, {depths, (size_t)tokens * 4, "depths"}};
+  const basa_status s = check_apart(in, 2, out, 2);
+  if (s != BASA_OK || tokens == 0) return s;
+  return launch_tree_masks(parents, cu_seqlens, n_seq, tokens, masks, words, mask_stride, depths, reinterpret_cast<hipStream_t>(stream));
+}
+
+size_t basa_tree_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t n_seq, int32_t width) {
+  if (check_tree(q, k_pages, v_pages, n_seq, width) != BASA_OK) return 0;
+  return tree_workspace_bytes(q->L, n_seq, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
+}
+
+basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                           int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
+                           int32_t words, int64_t mask_stride, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,
+                           void* stream) {
+  basa_status s;
+  if ((s = check_tree(q, k_pages, v_pages, n_seq, width)) != BASA_OK) return s;
+  if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
+  if (!cu_seqlens || (n_seq > 0 && !lens)) { set_error("null lens or cu_seqlens"); return BASA_ERR_INVALID_ARG; }
+  if (masks && (words < 1 || mask_stride < words || reinterpret_cast<uintptr_t>(masks) % 8)) {
+    set_error("masks: rows of %d words, %lld apart, 8-byte aligned", words, (long long)mask_stride); return BASA_ERR_INVALID_ARG;
+  }
+  if (!out) { set_error("null output pointer"); return BASA_ERR_INVALID_ARG; }
+  if (reinterpret_cast<uintptr_t>(out) % 16) { set_error("out must be 16-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  int64_t out_t = (int64_t)q->heads * q->d, out_h = q->d;
+  if (out_strides) {
+    const int64_t per16 = q->dtype == BASA_BF16 ? 8 : 4;
+    out_t = out_strides[0]; out_h = out_strides[1];
+    if (out_h < q->d || out_h % per16 || out_t % per16 || out_t < 0) {
+      set_error("out_strides must be non-negative multiples of 16 bytes with the head stride >= d");
+      return BASA_ERR_INVALID_ARG;
+    }
+  }
+  const size_t need = tree_workspace_bytes(q->L, n_seq, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
+  if (!ws || ws_bytes < need) {
+    set_error("tree workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
+    return BASA_ERR_WORKSPACE;
+  }
+  if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  return launch_tree_attn(view_of(*q), view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, cu_seqlens, n_seq, masks, words,
+                          mask_stride, out, out_t, out_h, lse, ws, reinterpret_cast<hipStream_t>(stream));
+}
+
+basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
+                               const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,
+                               void* stream) {
+  basa_status s;
+  if ((s = check_pages(k_pages, v_pages)) != BASA_OK) return s;
+  if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
+  if (most < 0 || keep_stride < most) { set_error("rows of keep are %lld entries apart, %d wide", (long long)keep_stride, most); return BASA_ERR_INVALID_ARG; }
+  if (n_seq > 0 && most > 0 && (!start || !keep || !count)) { set_error("null start, keep or count"); return BASA_ERR_INVALID_ARG; }
+  return launch_cache_compact(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, start, keep, most, keep_stride, count, n_seq,
+                              reinterpret_cast<hipStream_t>(stream));
+}
+
+basa_status basa_page_fork(const int32_t* table, int32_t width, int64_t table_stride, const int32_t* lens, int32_t n_seq, int32_t page,
+                           const int32_t* parents, int32_t n_new, const int32_t* free_pages, int32_t n_free, int32_t* new_table,
+                           int64_t new_stride, int32_t* new_lens, int32_t* copies, int32_t* pages, void* stream) {
+  basa_status s;
+  if (page < 1) { set_error("page size %d must be >= 1", page); return BASA_ERR_INVALID_ARG; }
+  if ((s = check_table(table, n_seq, width, table_stride, page)) != BASA_OK) return s;
+  if ((s = check_table(new_table, n_new, width, new_stride, page)) != BASA_OK) return s;
+  if (!page_fork_takes(n_seq, n_new)) { set_error("more sequences (%d, %d) than a call takes", n_seq, n_new); return BASA_ERR_UNSUPPORTED; }
+  if (n_seq > 0 && !lens) { set_error("null lens"); return BASA_ERR_INVALID_ARG; }
+  if (n_new > 0 && (!parents || !new_lens || !copies)) { set_error("null parents, new_lens or copies"); return BASA_ERR_INVALID_ARG; }
+  if (!pages) { set_error("null pages"); return BASA_ERR_INVALID_ARG; }
+  if (n_free < 0 || (n_free > 0 && !free_pages)) { set_error("null free_pages, or a negative number of them (%d)", n_free); return BASA_ERR_INVALID_ARG; }
+  const Span in[] = {{table, rows_span(n_seq, table_stride, width, 4), "table"}, {lens, (size_t)n_seq * 4, "lens"}, {parents, (size_t)n_new * 4, "parents"},
+                     {free_pages, (size_t)n_free * 4, "free_pages"}};
+  const Span out[] = {{new_table, rows_span(n_new, new_stride, width, 4), "new_table"}, {new_lens, (size_t)n_new * 4, "new_lens"},
+                      {copies, (size_t)n_new * 12, "copies"}, {pages, 8, "pages"}};
+  if ((s = check_apart(in, 4, out, 4)) != BASA_OK) return s;
+  return launch_page_fork(table, width, table_stride, lens, n_seq, page, parents, n_new, free_pages, n_free, new_table, new_stride, new_lens, copies,
+                          pages, reinterpret_cast<hipStream_t>(stream));
+}
+
+basa_status basa_cache_copy(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* copies, int32_t n, void* stream) {
+  const basa_status s = check_pages(k_pages, v_pages);
+  if (s != BASA_OK) return s;
+  if (n < 0 || (n > 0 && !copies)) { set_error("null copies, or a negative number of them (%d)", n); return BASA_ERR_INVALID_ARG; }
+  if ((int64_t)k_pages->L * k_pages->heads * 32 > INT32_MAX || n > kMaxDecodeRows) {
+    set_error("pages of %d tokens of %d heads, %d copies: more than a call takes", k_pages->L, k_pages->heads, n); return BASA_ERR_UNSUPPORTED;
+  }
+  return launch_cache_copy(view_of(*k_pages), view_of(*v_pages), copies, n, reinterpret_cast<hipStream_t>(stream));
+}
+
+namespace {
+basa_status check_free(int32_t n_seq, int32_t width, int32_t n_pages) {
+  if (n_seq < 0 || width < 1) { set_error("a block table of %d rows, %d wide", n_seq, width); return BASA_ERR_INVALID_ARG; }
+  if (n_pages < 1) { set_error("a cache has pages (got %d)", n_pages); return BASA_ERR_INVALID_ARG; }
+  if (n_pages > kMaxPagedTokens || n_seq > kMaxDecodeRows) { set_error("%d pages, %d sequences: more than a call takes", n_pages, n_seq); return BASA_ERR_UNSUPPORTED; }
+  return BASA_OK;
+}
+}  // namespace
+size_t basa_page_free_workspace_size(int32_t n_seq, int32_t width, int32_t n_pages) {
+  return check_free(n_seq, width, n_pages) == BASA_OK ? page_free_workspace_bytes(n_seq, width, n_pages) : 0;
+}
+basa_status basa_page_free(const int32_t* table, int32_t width, int64_t table_stride, const int32_t* lens, int32_t n_seq, int32_t page,
+                           int32_t n_pages, int32_t* free_pages, int32_t* count, void* ws, size_t ws_bytes, void* stream) {
+  basa_status s;
+  if (page < 1) { set_error("page size %d must be >= 1", page); return BASA_ERR_INVALID_ARG; }
+  if ((s = check_table(table, n_seq, width, table_stride, page)) != BASA_OK) return s;
+  if ((s = check_free(n_seq, width, n_pages)) != BASA_OK) return s;
+  if ((n_seq > 0 && !lens) || !free_pages || !count) { set_error("null lens, free_pages or count"); return BASA_ERR_INVALID_ARG; }
+  const size_t need = page_free_workspace_bytes(n_seq, width, n_pages);
+  if (!ws || ws_bytes < need) {
+    set_error("workspace too small: need %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
+    return BASA_ERR_WORKSPACE;
+  }
+  if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  const Span in[] = {{table, rows_span(n_seq, table_stride, width, 4), "table"}, {lens, (size_t)n_seq * 4, "lens"}};
+  const Span out[] = {{free_pages, (size_t)n_pages * 4, "free_pages"}, {count, 4, "count"}, {ws, need, "the workspace"}};
+  if ((s = check_apart(in, 2, out, 3)) != BASA_OK) return s;
+  return launch_page_free(table, width, table_stride, lens, n_seq, page, n_pages, free_pages, count, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

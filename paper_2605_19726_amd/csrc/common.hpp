@@ -42,7 +42,7 @@ basa_status hip_fail(hipError_t e, const char* what);
 // with a pair of HIP events on the launch stream when profiling is enabled.
 enum KernelId {
   K_NORM_TILE_SORT = 0, K_MERGE, K_STATS, K_SCORES, K_ROW_SELECT, K_GATHER, K_ATTN,
-  K_ATTN_F32, K_BLOCK_MASS, K_DIAG_SMALL, K_SCORES_SELECT, K_ATTN_COMBINE, K_PAGED, K_DECODE, K_DECODE_JOIN, K_COUNT
+  K_ATTN_F32, K_BLOCK_MASS, K_DIAG_SMALL, K_SCORES_SELECT, K_ATTN_COMBINE, K_PAGED, K_DECODE, K_DECODE_JOIN, K_TREE, K_TREE_JOIN, K_COUNT
 };
 struct ProfScope {
   ProfScope(int id, hipStream_t st);
@@ -190,6 +190,27 @@ size_t decode_workspace_bytes(int batch, int heads_q, int heads_kv, int d, bool 
 basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                                int64_t table_stride, const int32_t* lens, void* out, int64_t out_sb, int64_t out_sh, float* lse, void* ws,
                                hipStream_t st);
+
+// Several new tokens of every sequence (attn_tree.hip), and the pages around them (page_ops.hip).
+bool tree_takes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
+size_t tree_workspace_bytes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
+basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
+                             int64_t table_stride, const int32_t* lens, const int32_t* cu, int n, const int64_t* masks, int words,
+                             int64_t mask_stride, void* out, int64_t out_st, int64_t out_sh, float* lse, void* ws, hipStream_t st);
+constexpr int kMaxMaskWords = 64;
+basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, int tokens, int64_t* masks, int words, int64_t mask_stride,
+                              int32_t* depths, hipStream_t st);
+basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
+                                 const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
+                                 hipStream_t st);
+bool page_fork_takes(int n_old, int n_new);
+basa_status launch_page_fork(const int32_t* table, int width, int64_t table_stride, const int32_t* lens, int n_old, int page,
+                             const int32_t* parents, int n_new, const int32_t* free_pages, int n_free, int32_t* new_table, int64_t new_stride,
+                             int32_t* new_lens, int32_t* copies, int32_t* pages, hipStream_t st);
+basa_status launch_cache_copy(const TensorView& k_pages, const TensorView& v_pages, const int32_t* copies, int n, hipStream_t st);
+size_t page_free_workspace_bytes(int n_seq, int width, int n_pages);
+basa_status launch_page_free(const int32_t* table, int width, int64_t table_stride, const int32_t* lens, int n_seq, int page, int n_pages,
+                             int32_t* free_pages, int32_t* count, void* ws, hipStream_t st);
 
 // Selection-fidelity diagnostics (diag.hip).  block mass: bf16 on the matrix cores, f32 on a plain kernel.
 size_t block_mass_workspace_bytes(int BHq, int BHkv, int Lq, int Lk, int d);

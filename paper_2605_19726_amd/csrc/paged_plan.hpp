@@ -50,8 +50,8 @@ BASA_HD int decode_run(int total) {          // total < 2^31 - kDecodeMost
 }
 // What lies in a run of a (sequence, head) whose first place is `first`: steps [t0, t1), none if t1 <= t0.
 struct DecodePiece { int t0, t1; };
-BASA_HD DecodePiece decode_piece(int first, int steps, int group, int run) {
-  const int64_t begin = (int64_t)group * run - first - kDecodeLead, end = begin + run;
+BASA_HD DecodePiece decode_piece(int first, int steps, int group, int run, int lead = kDecodeLead) {
+  const int64_t begin = (int64_t)group * run - first - lead, end = begin + run;
   DecodePiece p;
   p.t0 = begin > 0 ? (int)(begin < steps ? begin : steps) : 0;
   p.t1 = end < steps ? (end > 0 ? (int)end : 0) : steps;
@@ -61,9 +61,28 @@ BASA_HD DecodePiece decode_piece(int first, int steps, int group, int run) {
 // partial results, and the beginning of one that goes on behind it, place 1.
 BASA_HD int decode_part(DecodePiece p, int group) { return 2 * group + (p.t0 == 0 ? 1 : 0); }
 // The groups that have steps of it: first and last.
-BASA_HD int decode_first_group(int first, int run) { return (first + kDecodeLead) / run; }
-BASA_HD int decode_last_group(int first, int steps, int run) { return (first + kDecodeLead + steps - 1) / run; }
+BASA_HD int decode_first_group(int first, int run, int lead = kDecodeLead) { return (first + lead) / run; }
+BASA_HD int decode_last_group(int first, int steps, int run, int lead = kDecodeLead) { return (first + lead + steps - 1) / run; }
 // Workgroups of a call of up to `most` places, whatever the lengths turn out to be.
 inline int decode_groups(int64_t most) { return (int)(most < kDecodeMost ? most : kDecodeMost); }
+
+// ---- several new tokens of every sequence -----------------------------------------------------------
+// The same axis for attention whose rows are (new token, query head) pairs: a (sequence, KV head) has a unit for every `tile` of its rows, none if
+// there are none; the units lie in the order sequence, head, tile, each with places as above, for steps of `step` tokens.
+BASA_HD constexpr int tree_lead(int step) { return step < kDecodeStep ? kDecodeStep / step : 1; }
+BASA_HD int tree_steps(int len, int step) { return len <= step ? 1 : (len + step - 1) / step; }
+BASA_HD int tree_units(int rows, int tile) { return (rows + tile - 1) / tile; }
+// What 32 drafted tokens from `at` on (negative: tokens of the context, which all see) the token `t` of a chain sees: those up to itself.
+BASA_HD uint32_t chain_bits(int t, int at) {
+  const int count = t - at + 1;
+  return count <= 0 ? 0u : count >= 32 ? ~0u : (1u << count) - 1u;
+}
+// The same of the masks of a tree: the 64-bit words that hold bits at / 64 and at / 64 + 1 (zero where there is none; of at < 0: `low` is word 0).
+BASA_HD uint32_t tree_bits(uint64_t low, uint64_t high, int at) {
+  if (at <= -32) return ~0u;
+  if (at < 0) return (uint32_t)(low << -at) | ((1u << -at) - 1u);
+  const int s = at & 63;
+  return (uint32_t)(s > 32 ? (low >> s) | (high << (64 - s)) : low >> s);
+}
 
 }  // namespace basa
