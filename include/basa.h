@@ -391,7 +391,8 @@ basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, i
  *   ws           workspace of basa_tree_workspace_size() bytes.  Nothing in it has to start at zero.
  * Tokens that a query does not see, or whose page is none, carry no weight, whatever their rows hold; a query without any token gets a zero row and lse = -inf, as
  * does one whose scores are all -inf.  Infinite values, accuracy and splitting as with basa_decode_attn; how rows are put together goes by T and n_seq too.
- * Pages and tokens of a cache lie less than 2^36 bytes apart.
+ * K and V each reach over less than 2^32 times the largest power of two, up to 256 bytes, that divides their pages' and tokens' strides (BASA_ERR_UNSUPPORTED):
+ * 512 GiB and more for stores of whole rows.
  */
 size_t basa_tree_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t n_seq, int32_t width);
 basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,

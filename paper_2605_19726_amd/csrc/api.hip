@@ -429,11 +429,7 @@ basa_status check_tree(const basa_tensor* q, const basa_tensor* k, const basa_te
   }
   if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
   if ((int64_t)q->L * q->heads > kMaxTreeRows) { set_error("q: tokens*heads exceeds %d", kMaxTreeRows); return BASA_ERR_UNSUPPORTED; }
-  const int64_t most = (int64_t)1 << 36, e = q->dtype == BASA_BF16 ? 2 : 4;
-  for (const basa_tensor* t : {k, v})
-    if (t->stride_b * e >= most || t->stride_l * e >= most) {
-      set_error("pages or tokens of a cache lie %lld bytes apart or more", (long long)most); return BASA_ERR_UNSUPPORTED;
-    }
+  if (tree_place_unit(view_of(*k), view_of(*v)) < 0) { set_error("pages that reach further than the tokens' places do (2^32 times a row)"); return BASA_ERR_UNSUPPORTED; }
   if ((s = check_width(width, k->L)) != BASA_OK) return s;
   if (!tree_takes(q->L, n_seq, q->heads, k->heads, q->d, q->dtype == BASA_BF16, width * k->L)) {
     set_error("%d new tokens of %d sequences with room for %lld tokens each: more steps than a call takes", q->L, n_seq, (long long)width * k->L);

@@ -20,14 +20,15 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
 typedef const __attribute__((address_space(3))) char* lds_cptr_t;
-typedef const __attribute__((address_space(3))) uintx4* lds_chunk_ptr_t;
+typedef __attribute__((address_space(3))) uintx4* lds_chunk_ptr_t;
 typedef __attribute__((address_space(3))) short4v* lds_quad_ptr_t;
 
 struct TreeArgs {
   const char *q, *k, *v;
   int64_t q_t, q_h;                         // strides in bytes
   int64_t k_h, v_h;
-  uint32_t k_b, k_l, v_b, v_l;              // of a page and of a token, in units of 16 bytes
+  uint32_t k_b, k_l, v_b, v_l;              // of a page and of a token, in units of 2^unit bytes
+  int unit;
   const int32_t *table, *lens, *cu;
   int64_t table_stride;
   int n, tokens, heads_kv, group, pages;    // sequences; rows of q
@@ -46,12 +47,11 @@ struct TreeArgs {
   float2* part_ml;                          // [2 runs][tile] maximum in units of the exponent, sum
   float scale_log2e;                        // log2 e / sqrt(d)
 };
-__device__ const uint4 kZeroRow[32] = {};   // the row of a token whose page is none
-
-constexpr int kWaves = 4, kThreads = 64 * kWaves;
-constexpr int kTile = 32;                   // tokens that a wave takes at a time
 constexpr int kPlanBatch = 512;             // up to this many sequences every wave sums up the lengths by itself
-constexpr int kWindow = 1024, kWindowPages = kWindow + 4;     // tokens whose page ids are in the LDS, twice
+constexpr int kWindow = 256;                // tokens whose places in the cache are in the LDS, twice
+// How far a row's scores, in units of the exponent, may rise above the maximum that its weights refer to before these are scaled: weights up to 2^8 are as exact as
+// weights up to 1.
+constexpr float kRise = 8.f;
 
 struct Sequence { int len, row0, n; };
 __device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
@@ -89,15 +89,15 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
     *reinterpret_cast<floatx4*>(at) = o;
   }
 }
-// p times this lies 3/4 to 3/2 steps of bf16 below p, so that its rounding is below p and the rest is positive.
-constexpr float kBelow = 1.f - 0x3p-9f;
-
 // 16 bytes from memory for every lane, side by side into the LDS.  Written in assembly, without a register for its result: the compiler would wait for all of
 // these before it reads the LDS or meets a barrier; the waits stand where the ring needs them.
 template <bool kOnce>
 __device__ __forceinline__ void to_lds(const char* from, uint32_t at) {
   if constexpr (kOnce) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(at) : "memory");
   else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "memory");
+}
+__device__ __forceinline__ void word_to_lds(const void* from, uint32_t at) {      // 4 bytes for every lane
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at) : "memory");
 }
 // Everyone's LDS operations are done before anyone goes on.  Requests by to_lds that are under way stay so.
 __device__ __forceinline__ void meet() {
@@ -112,7 +112,10 @@ __device__ __forceinline__ bf16x4 lds_turned(uint32_t at) {
   return __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad_ptr_t)(uintptr_t)at));
 }
 
-// What a wave does with 32 tokens in the LDS for its rows.  Row of a lane: its column of the matrix instruction.
+// Whether there are tokens of a step that the lane's row does not see, and bits of those that it does.
+struct Seen { bool masked; uint32_t bits; };
+
+// What a wave does with a step's tokens in the LDS for its rows.  Row of a lane: its column of the matrix instruction.
 template <bool kBf16, int kD> struct Rows;
 
 // bf16: 32 rows, 32x32x16 instructions.  S^T = K Q^T: lane (h, r) of the A operand holds chunk 2 c + h of token r at step c.  Of the result lane (h, n) holds
@@ -120,7 +123,7 @@ template <bool kBf16, int kD> struct Rows;
 // 8 h + 4 w + j of the sum.  The A operand in that order: the transposing read gives lane i of 16 column i of the four rows that they address.
 template <int kD>
 struct Rows<true, kD> {
-  static constexpr int kRows = 32, kKSteps = kD / 16, kBlocks = kD / 32, kRowBytes = kD * 2, kChunks = kRowBytes / 16;
+  static constexpr int kRows = 32, kTokens = 32, kKSteps = kD / 16, kBlocks = kD / 32, kRowBytes = kD * 2, kChunks = kRowBytes / 16;
   uintx4 q[kKSteps];
   floatx16 acc[kBlocks];
   float m, l;                               // maximum in units of the exponent, the lane's part of the sum
@@ -144,7 +147,7 @@ struct Rows<true, kD> {
     const int i = lane & 15, row = 4 * (lane >> 5) + (i >> 2);
     return row * kRowBytes + v_place(row, 2 * (lane >> 4 & 1) + (i >> 1 & 1)) * 16 + (i & 1) * 8;
   }
-  // The operand of tokens 16 u .. of the wave's 32, dimensions 32 e ..
+  // The operand of tokens 16 u .., dimensions 32 e ..
   static __device__ __forceinline__ bf16x8 v_operand(uint32_t v_lds, int u, int e) {
     bf16x8 f;
 #pragma unroll
@@ -155,24 +158,44 @@ struct Rows<true, kD> {
     }
     return f;
   }
-  // kMasked: `seen` has a bit for every token that the lane's row sees.  kSafe: see below.
-  template <bool kMasked, bool kSafe>
-  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, uint32_t seen, float scale, int lane) {
-    const int h = lane >> 5;
-    floatx16 s = floatx16{0};
+  // Scores; -inf where `seen` says so.  meanwhile(): what is done while the matrix instructions run, and gives `seen`.
+  template <class F>
+  __device__ __forceinline__ void scores(floatx16& s, uint32_t k_lds, int lane, F meanwhile) const {
+    s = floatx16{0};
+    uintx4 k[kKSteps];
+#pragma unroll
+    for (int c = 0; c < kKSteps; ++c) k[c] = lds_chunk(k_lds ^ (32 * c));
+    __builtin_amdgcn_sched_barrier(0);          // all of them on their way before the first is waited for
 #pragma unroll
     for (int c = 0; c < kKSteps; ++c)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lds_chunk(k_lds ^ (32 * c))), __builtin_bit_cast(bf16x8, q[c]), s, 0, 0, 0);
-    if constexpr (kMasked) {
-      const uint32_t mine = seen >> (4 * h);
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, k[c]), __builtin_bit_cast(bf16x8, q[c]), s, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    const Seen seen = meanwhile();
+    if (seen.masked) {
+      asm volatile("");                         // (a branch: few steps go this way, and as selects it is a third of the instructions)
+      const uint32_t mine = seen.bits >> (4 * (lane >> 5));
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = mine >> (8 * (i >> 2) + (i & 3)) & 1 ? s[i] : -INFINITY;
     }
+  }
+  template <class F>
+  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, int lane, F meanwhile) {
+    floatx16 s;
+    bf16x8 v[2][kBlocks];
+    scores(s, k_lds, lane, [&] {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < kBlocks; ++e) v[u][e] = v_operand(v_lds, u, e);
+      const Seen seen = meanwhile();
+      __builtin_amdgcn_sched_barrier(0);
+      return seen;
+    });
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(pair_max<32>(top) * scale, m);
-    if (__ballot(top != m)) {
+    if (__ballot(top > m + kRise)) {
       const float f = factor_of(m, top);
       m = top;
       l *= f;
@@ -184,62 +207,65 @@ struct Rows<true, kD> {
     uint32_t hi[8], lo[8];
 #pragma unroll
     for (int i = 0; i < 16; i += 2) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
       float p[2];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         p[x] = __builtin_amdgcn_exp2f(fmaf(s[i + x], scale, -base));
         sum += p[x];
       }
-      uint32_t b0, b1;
-      if constexpr (kSafe) {
-        b0 = __float_as_uint((float)(__bf16)(p[0] * kBelow));
-        b1 = __float_as_uint((float)(__bf16)(p[1] * kBelow));
-      } else {
-        b0 = __float_as_uint(p[0]) & 0xffff0000u;
-        b1 = __float_as_uint(p[1]) & 0xffff0000u;
-      }
+      const uint32_t b0 = __float_as_uint(p[0]), b1 = __float_as_uint(p[1]);
       hi[i / 2] = __builtin_amdgcn_perm(b1, b0, 0x07060302);
-      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-      const bf16x2 rest = {(__bf16)(p[0] - __uint_as_float(b0)), (__bf16)(p[1] - __uint_as_float(b1))};
+      const bf16x2 rest = {(__bf16)(p[0] - __uint_as_float(b0 & 0xffff0000u)), (__bf16)(p[1] - __uint_as_float(b1 & 0xffff0000u))};
       lo[i / 2] = __builtin_bit_cast(uint32_t, rest);
     }
     l += sum;
-    bf16x8 ph[2], pl[2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      ph[u] = __builtin_bit_cast(bf16x8, uintx4{hi[4 * u], hi[4 * u + 1], hi[4 * u + 2], hi[4 * u + 3]});
-      pl[u] = __builtin_bit_cast(bf16x8, uintx4{lo[4 * u], lo[4 * u + 1], lo[4 * u + 2], lo[4 * u + 3]});
+      const bf16x8 ph = __builtin_bit_cast(bf16x8, uintx4{hi[4 * u], hi[4 * u + 1], hi[4 * u + 2], hi[4 * u + 3]});
+      const bf16x8 pl = __builtin_bit_cast(bf16x8, uintx4{lo[4 * u], lo[4 * u + 1], lo[4 * u + 2], lo[4 * u + 3]});
+#pragma unroll
+      for (int e = 0; e < kBlocks; ++e) {
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u][e], ph, acc[e], 0, 0, 0);
+        acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[u][e], pl, acc[e], 0, 0, 0);
+      }
     }
-    if constexpr (kMasked && kSafe) {
-      // token by token, added where it is seen: what a row does not see may be anything
+  }
+  // Bits of the tokens whose weight is not zero.
+  __device__ __forceinline__ uint32_t weighs(uint32_t k_lds, Seen seen, float scale, int lane) const {
+    floatx16 s;
+    scores(s, k_lds, lane, [&] { return seen; });
+    const float base = exponent_base(m);
+    uint32_t bits = 0, other, mine;
 #pragma unroll
-      for (int e = 0; e < kBlocks; ++e)
+    for (int i = 0; i < 16; ++i)
+      if (__builtin_amdgcn_exp2f(fmaf(s[i], scale, -base)) != 0.f) bits |= 1u << (8 * (i >> 2) + (i & 3));
+    lane_pair<32>(bits << (4 * (lane >> 5)), mine, other);
+    return mine | other;
+  }
+  // The values of a token (number `row` in the LDS) that are not finite, with weight `on` (NaN if that is zero).
+  __device__ __forceinline__ void add_not_finite(uint32_t v_stage, int row, bool seen, bool on, int lane) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          const bf16x8 v = v_operand(v_lds, u, e);
-#pragma clang loop unroll(disable)
-          for (int t = 0; t < 16; ++t) {
-            bf16x8 one;
+    for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) one[i] = t == 8 * (i >> 2) + 4 * h + (i & 3) ? v[i] : (__bf16)0.f;
-            floatx16 x = floatx16{0};
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, ph[u], x, 0, 0, 0);
-            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(one, pl[u], x, 0, 0, 0);
-            const bool on = seen >> (16 * u + t) & 1;
+      for (int q4 = 0; q4 < 4; ++q4) {
+        const int dim = 32 * e + 8 * q4 + 4 * (lane >> 5);
+        const uintx4 v = lds_chunk(v_stage + row * kRowBytes + v_place(row, dim / 8) * 16);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[e][i] = on ? acc[e][i] + x[i] : acc[e][i];
-          }
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t w = lane >> 5 ? v[2 + j / 2] : v[j / 2], x = j & 1 ? w & 0xffff0000u : w << 16;
+          if ((x & 0x7f800000u) == 0x7f800000u) acc[e][4 * q4 + j] += seen ? on ? __uint_as_float(x) : NAN : 0.f;
         }
-    } else {
+      }
+  }
+  // A chunk of values without those that are not finite.
+  static __device__ __forceinline__ uintx4 finite(uintx4 v) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < kBlocks; ++e) {
-          const bf16x8 v = v_operand(v_lds, u, e);
-          acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, ph[u], acc[e], 0, 0, 0);
-          acc[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, pl[u], acc[e], 0, 0, 0);
-        }
+    for (int i = 0; i < 4; ++i) {
+      if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] &= 0x0000ffffu;
+      if ((v[i] & 0x00007f80u) == 0x00007f80u) v[i] &= 0xffff0000u;
     }
+    return v;
   }
   __device__ __forceinline__ bool any_nan() const {
     float x = 0.f;
@@ -251,23 +277,22 @@ struct Rows<true, kD> {
   }
   __device__ __forceinline__ float whole_sum() const { return pair_sum<32>(l); }
   static __device__ __forceinline__ bool writes_sum(int lane) { return lane < 32; }
-  template <int kPitch>
-  __device__ __forceinline__ void store(float* part, int lane) const {       // to row column(lane) of `part`
-    float* row = part + (lane & 31) * kPitch + 4 * (lane >> 5);
+  // f(first of four dimensions, their sums) for all that a lane has of its row.
+  template <class F>
+  __device__ __forceinline__ void each(int lane, F f) const {
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<floatx4*>(row + 32 * e + 8 * q4) = floatx4{acc[e][4 * q4], acc[e][4 * q4 + 1], acc[e][4 * q4 + 2], acc[e][4 * q4 + 3]};
+      for (int i = 0; i < 16; i += 4) f(32 * e + 2 * i + 4 * (lane >> 5), floatx4{acc[e][i], acc[e][i + 1], acc[e][i + 2], acc[e][i + 3]});
   }
 };
 
-// f32: 16 rows, 16x16x4 instructions, the tokens in two halves of 16.  S^T = K Q^T: lane (g, r) holds chunk 4 c + g of token r, four products; the score is the sum
-// of four sums of d / 4.  Of the result lane (g, n) holds tokens 4 g + j of row n: the B operand of O^T += V^T P^T for tokens j, 4 + j, 8 + j, 12 + j.  The A
-// operand: lane (g, r) holds dimensions 64 x + 4 r .. of token 4 g + j; output block 4 x + y has dimensions 64 x + 4 r + y.
+// f32: 16 rows, 16x16x4 instructions, 16 tokens.  S^T = K Q^T: lane (g, r) holds chunk 4 c + g of token r, four products; the score is the sum of four sums of d / 4.
+// Of the result lane (g, n) holds tokens 4 g + j of row n: the B operand of O^T += V^T P^T for tokens j, 4 + j, 8 + j, 12 + j.  The A operand: lane (g, r)
+// holds dimensions 64 x + 4 r .. of token 4 g + j; output block 4 x + y has dimensions 64 x + 4 r + y.
 template <int kD>
 struct Rows<false, kD> {
-  static constexpr int kRows = 16, kKSteps = kD / 16, kBlocks = kD / 16, kRowBytes = kD * 4, kChunks = kRowBytes / 16;
+  static constexpr int kRows = 16, kTokens = 16, kKSteps = kD / 16, kBlocks = kD / 16, kRowBytes = kD * 4, kChunks = kRowBytes / 16;
   uintx4 q[kKSteps];
   floatx4 acc[kBlocks];
   float m, l;
@@ -288,33 +313,43 @@ struct Rows<false, kD> {
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e) acc[e] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
-  template <bool kMasked, bool kSafe>
-  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, uint32_t seen, float scale, int lane) {
-    const int g = lane >> 4;
-    floatx4 s[2];
+  template <class F>
+  __device__ __forceinline__ void scores(floatx4& s, uint32_t k_lds, int lane, F meanwhile) const {
+    floatx4 x[4] = {};
+    uintx4 k[kKSteps];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      floatx4 x[4] = {};
+    for (int c = 0; c < kKSteps; ++c) k[c] = lds_chunk(k_lds ^ (64 * c));
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int c = 0; c < kKSteps; ++c) {
-        const uintx4 k = lds_chunk((k_lds ^ (64 * c)) + 16 * half * kRowBytes);
+    for (int c = 0; c < kKSteps; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[e]), __uint_as_float(q[c][e]), x[e], 0, 0, 0);
-      }
-      s[half] = (x[0] + x[1]) + (x[2] + x[3]);
-      if constexpr (kMasked) {
-        const uint32_t mine = seen >> (16 * half + 4 * g);
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k[c][e]), __uint_as_float(q[c][e]), x[e], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    const Seen seen = meanwhile();
+    s = (x[0] + x[1]) + (x[2] + x[3]);
+    if (seen.masked) {
+      asm volatile("");
+      const uint32_t mine = seen.bits >> (4 * (lane >> 4));
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[half][j] = mine >> j & 1 ? s[half][j] : -INFINITY;
-      }
+      for (int j = 0; j < 4; ++j) s[j] = mine >> j & 1 ? s[j] : -INFINITY;
     }
-    float top = -INFINITY;
+  }
+  template <class F>
+  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, int lane, F meanwhile) {
+    floatx4 s;
+    uintx4 v[4][kD / 64];
+    scores(s, k_lds, lane, [&] {
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+      for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) top = fmaxf(top, s[half][j]);
+        for (int x = 0; x < kD / 64; ++x) v[j][x] = lds_chunk(v_lds + j * kRowBytes + 256 * x);
+      const Seen seen = meanwhile();
+      __builtin_amdgcn_sched_barrier(0);
+      return seen;
+    });
+    float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     top = fmaxf(pair_max<16>(pair_max<32>(top)) * scale, m);
-    if (__ballot(top != m)) {
+    if (__ballot(top > m + kRise)) {
       const float f = factor_of(m, top);
       m = top;
       l *= f;
@@ -324,36 +359,46 @@ struct Rows<false, kD> {
     const float base = exponent_base(m);
     float sum = 0.f;
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[half][j] = __builtin_amdgcn_exp2f(fmaf(s[half][j], scale, -base));
-        sum += s[half][j];
-      }
+    for (int j = 0; j < 4; ++j) {
+      s[j] = __builtin_amdgcn_exp2f(fmaf(s[j], scale, -base));
+      sum += s[j];
+    }
     l += sum;
 #pragma unroll
-    for (int half = 0; half < 2; ++half)
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int x = 0; x < kD / 64; ++x)
 #pragma unroll
-        for (int x = 0; x < kD / 64; ++x) {
-          const uintx4 v = lds_chunk(v_lds + (16 * half + j) * kRowBytes + 256 * x);
+        for (int y = 0; y < 4; ++y) acc[4 * x + y] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[j][x][y]), s[j], acc[4 * x + y], 0, 0, 0);
+  }
+  __device__ __forceinline__ uint32_t weighs(uint32_t k_lds, Seen seen, float scale, int lane) const {
+    floatx4 s;
+    scores(s, k_lds, lane, [&] { return seen; });
+    const float base = exponent_base(m);
+    uint32_t bits = 0, x, y;
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            floatx4& o = acc[4 * x + y];
-            if constexpr (kMasked && kSafe) {
-#pragma clang loop unroll(disable)
-              for (int t = 0; t < 4; ++t) {
-                const floatx4 one = __builtin_amdgcn_mfma_f32_16x16x4f32(t == g ? __uint_as_float(v[y]) : 0.f, s[half][j], floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-                const bool on = seen >> (16 * half + 4 * t + j) & 1;
+    for (int j = 0; j < 4; ++j)
+      if (__builtin_amdgcn_exp2f(fmaf(s[j], scale, -base)) != 0.f) bits |= 1u << j;
+    lane_pair<32>(bits << (4 * (lane >> 4)), x, y);
+    lane_pair<16>(x | y, x, y);
+    return x | y;
+  }
+  __device__ __forceinline__ void add_not_finite(uint32_t v_stage, int row, bool seen, bool on, int lane) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = on ? o[i] + one[i] : o[i];
-              }
-            } else {
-              o = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(v[y]), s[half][j], o, 0, 0, 0);
-            }
-          }
-        }
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < kD / 64; ++x) {
+        const uintx4 v = lds_chunk(v_stage + row * kRowBytes + 256 * x + (4 * (lane >> 4) + i) * 16);
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+          if ((v[y] & 0x7f800000u) == 0x7f800000u) acc[4 * x + y][i] += seen ? on ? __uint_as_float(v[y]) : NAN : 0.f;
+      }
+  }
+  static __device__ __forceinline__ uintx4 finite(uintx4 v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] = 0u;
+    return v;
   }
   __device__ __forceinline__ bool any_nan() const {
     float x = 0.f;
@@ -365,48 +410,51 @@ struct Rows<false, kD> {
   }
   __device__ __forceinline__ float whole_sum() const { return pair_sum<16>(pair_sum<32>(l)); }
   static __device__ __forceinline__ bool writes_sum(int lane) { return lane < 16; }
-  template <int kPitch>
-  __device__ __forceinline__ void store(float* part, int lane) const {
-    float* row = part + (lane & 15) * kPitch;
+  template <class F>
+  __device__ __forceinline__ void each(int lane, F f) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
       for (int x = 0; x < kD / 64; ++x)
-        *reinterpret_cast<floatx4*>(row + 64 * x + 4 * (4 * (lane >> 4) + i)) = floatx4{acc[4 * x][i], acc[4 * x + 1][i], acc[4 * x + 2][i], acc[4 * x + 3][i]};
+        f(64 * x + 4 * (4 * (lane >> 4) + i), floatx4{acc[4 * x][i], acc[4 * x + 1][i], acc[4 * x + 2][i], acc[4 * x + 3][i]});
   }
 };
 
-// kRowWaves waves side by side over the rows of a tile, the others over the tokens of a step.  Of a ring of kStages steps in the LDS one is worked on, the
-// others are on their way there.
-template <bool kBf16, int kD, int kRowWaves>
+// A workgroup has a wave for every kRows rows of a tile; each takes every token.  Of a ring of kStages steps in the LDS one is worked on, the others are on
+// their way there.
+template <bool kBf16, int kD, int kWaves>
 struct Geometry {
   using R = Rows<kBf16, kD>;
-  static constexpr int kTokenWaves = kWaves / kRowWaves, kStep = kTile * kTokenWaves, kRowTile = R::kRows * kRowWaves;
-  static constexpr int kHalfBytes = kStep * R::kRowBytes, kStageBytes = 2 * kHalfBytes;      // K, then V
-  static constexpr int kLoads = kHalfBytes / 1024 / kWaves;                                  // per wave, of K and of V each
-  static constexpr int kStages = kStageBytes >= 64 * 1024 ? 2 : kStageBytes >= 32 * 1024 ? 2 : 4;
-  static constexpr int kPitch = kD + 4;
-  static constexpr int kPartBytes = kWaves * R::kRows * kPitch * 4;
-  static constexpr int kIdsAt = kStages * kStageBytes;
-  static constexpr int kRingBytes = kIdsAt + 2 * kWindowPages * 4;
-  static constexpr int kMlAt = (kRingBytes > kPartBytes ? kRingBytes : kPartBytes) / 16 * 16 + 16;
-  static constexpr int kLdsBytes = kMlAt + kWaves * R::kRows * 8 + 16;       // then the vote, and whether a window has pages that are none
-  static constexpr int kGroups = kLdsBytes > 80 * 1024 ? 1 : 2;                // workgroups that a compute unit holds
+  static constexpr int kThreads = 64 * kWaves, kStep = R::kTokens, kRowTile = R::kRows * kWaves;
+  static constexpr int kHalfBytes = kStep * R::kRowBytes, kStageBytes = 2 * kHalfBytes;      // K, then V: 8 or 16 KB
+  static constexpr int kLoads = kStageBytes / 1024 / kWaves;                                 // of a wave for a step, 1 KB each
+  static constexpr bool kLarge = kStageBytes > 8 * 1024;
+  static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? (kLarge ? 4 : 8) : 4;
+  static constexpr int kGroups = kWaves == 8 ? 1 : kWaves == 4 ? 2 : kLarge ? 2 : 4;         // workgroups that a compute unit holds
+  static constexpr int kWavesPerSimd = (kGroups * kWaves + 3) / 4;
+  static constexpr int kPlacesAt = kStages * kStageBytes, kIdsAt = kPlacesAt + 2 * kWindow * 8;       // places of K and V, page ids
+  static constexpr int kLiveAt = kIdsAt + 2 * kWindow * 4, kVoteAt = kLiveAt + 2 * kWindow / 8, kLdsBytes = kVoteAt + 16;
+  static_assert(kGroups * kLdsBytes <= 160 * 1024, "the LDS");
 };
 
-template <bool kBf16, int kD, int kRowWaves, bool kSplit, bool kOnce>
-__global__ __launch_bounds__(kThreads, (Geometry<kBf16, kD, kRowWaves>::kGroups)) void tree_kernel(TreeArgs a) {
-  using G = Geometry<kBf16, kD, kRowWaves>;
+// All but the youngest `steps` requests of a wave have landed, of kLoads each; more than kMost are not waited for.
+template <int kMost, int kLoads>
+__device__ __forceinline__ void wait_for_all_but(int steps) {
+  if (steps >= kMost) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kMost * kLoads) : "memory");
+  else if constexpr (kMost > 0) wait_for_all_but<kMost - 1, kLoads>(steps);
+}
+
+template <bool kBf16, int kD, int kWaves, bool kSplit, bool kOnce>
+__global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPerSimd)) void tree_kernel(TreeArgs a) {
+  using G = Geometry<kBf16, kD, kWaves>;
   using R = Rows<kBf16, kD>;
-  constexpr int kElem = kBf16 ? 2 : 4, kLead = kSplit ? tree_lead(G::kStep) : 0;
+  constexpr int kElem = kBf16 ? 2 : 4, kLead = kSplit ? tree_lead(G::kStep) : 0, kThreads = G::kThreads;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   int* const ids = reinterpret_cast<int*>(smem + G::kIdsAt);
-  float* const part = reinterpret_cast<float*>(smem);
-  float2* const part_ml = reinterpret_cast<float2*>(smem + G::kMlAt);
-  int* const vote = reinterpret_cast<int*>(smem + G::kMlAt + kWaves * R::kRows * 8);
-  int* const holes = vote + 1;                    // [2]
+  uint2* const places_at = reinterpret_cast<uint2*>(smem + G::kPlacesAt);
+  uint64_t* const live_at = reinterpret_cast<uint64_t*>(smem + G::kLiveAt);      // bits of the tokens that there are
+  int* const vote = reinterpret_cast<int*>(smem + G::kVoteAt);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int row_wave = wave % kRowWaves, token_wave = wave / kRowWaves;
   auto places_of = [&](const Sequence& s) {       // of one unit
     return kSplit ? tree_steps(s.len, G::kStep) + kLead : 1;
   };
@@ -476,7 +524,7 @@ __global__ __launch_bounds__(kThreads, (Geometry<kBf16, kD, kRowWaves>::kGroups)
 
     R rw;
     const uint32_t ring = lds_address(smem), k_lane = R::k_at(lane), v_lane = R::v_at(lane);
-    const int row_first = row_wave * R::kRows;    // of the unit
+    const int row_first = wave * R::kRows;    // of the unit
     const bool works = row_first < unit_rows;
     const int my_row = unit * G::kRowTile + min(row_first + R::column(lane), unit_rows - 1);
     const int my_token = (int)a.per_token.div(my_row), my_head = kvh * a.group + my_row - my_token * a.group;
@@ -487,118 +535,147 @@ __global__ __launch_bounds__(kThreads, (Geometry<kBf16, kD, kRowWaves>::kGroups)
     const int32_t* const table = a.table + (int64_t)seq_b * a.table_stride;
     const char* const k_head = a.k + kvh * a.k_h;
     const char* const v_head = a.v + kvh * a.v_h;
-    auto fill = [&](int window) {                 // page ids of a window of tokens; everyone is there before and after
-      const int tok0 = window * kWindow, side = window & 1;
-      if (tid == 0) holes[side] = 0;
-      meet();
-      const int p0 = (int)a.page.div(tok0), p1 = (int)a.page.div(min(tok0 + kWindow, limit) - 1);
-      for (int i = tid; i <= p1 - p0; i += kThreads) {
-        const int id = table[p0 + i];
-        ids[side * kWindowPages + i] = id;
-        if ((unsigned)id >= (unsigned)a.pages) holes[side] = 1;
+    // Page ids of a window of tokens, on their way to the LDS like everything else; then their tokens' places.
+    auto fetch_ids = [&](int window) {
+      const int tok0 = window * kWindow, p0 = (int)a.page.div(min(tok0, limit - 1)), last = (int)a.page.div(limit - 1);
+      for (int i = wave; i < kWindow / 64; i += kWaves)
+        word_to_lds(table + min(p0 + 64 * i + lane, last), ring + G::kIdsAt + ((window & 1) * kWindow + 64 * i) * 4);
+    };
+    auto place_tokens = [&](int window) {         // everyone is there before and after
+      const int side = window & 1, tok0 = window * kWindow, p0 = (int)a.page.div(tok0);
+#pragma unroll
+      for (int at = tid; at < kWindow; at += kThreads) {
+        const int tok = min(tok0 + at, limit - 1), p = (int)a.page.div(tok), off = tok - p * (int)a.page.d;      // (behind the last: that one's place again)
+        const uint32_t id = ids[side * kWindow + p - p0];
+        const bool held = id < (uint32_t)a.pages;
+        places_at[side * kWindow + at] = held ? make_uint2(id * a.k_b + off * a.k_l, id * a.v_b + off * a.v_l) : make_uint2(0u, 0u);
+        const uint64_t live = __ballot(held && tok0 + at < limit);
+        if (lane == 0) live_at[(side * kWindow + at) >> 6] = live;
       }
-      meet();
     };
-    auto page_of = [&](int tok, int* off) {       // of tokens before `limit`: the id may be that of no page
-      const int p = (int)a.page.div(tok), p0 = (int)a.page.div(tok & ~(kWindow - 1));
-      *off = tok - p * (int)a.page.d;
-      return ids[((tok / kWindow) & 1) * kWindowPages + p - p0];
-    };
+    // What a lane fetches of a step: 16 bytes of K or V of a token in each of its wave's requests.
+    const char* from[G::kLoads];
+    int from_row[G::kLoads];
+    bool from_v[G::kLoads];
+#pragma unroll
+    for (int i = 0; i < G::kLoads; ++i) {
+      const int chunk = i * kWaves + wave, in_half = chunk % (G::kHalfBytes / 1024), c = lane % R::kChunks;
+      from_row[i] = in_half * (1024 / R::kRowBytes) + lane / R::kChunks;
+      from_v[i] = chunk >= G::kHalfBytes / 1024;
+      from[i] = from_v[i] ? v_head + R::v_place(from_row[i], c) * 16 : k_head + R::k_place(from_row[i], c) * 16;
+    }
     auto issue = [&](int step, int stage) {
 #pragma unroll
       for (int i = 0; i < G::kLoads; ++i) {
-        const int chunk = i * kWaves + wave, row = chunk * (1024 / R::kRowBytes) + lane / R::kChunks, c = lane % R::kChunks;
-        int off;
-        const int tok = step * G::kStep + row, id = page_of(min(tok, limit - 1), &off);
-        const bool valid = (unsigned)id < (unsigned)a.pages && tok < limit;
-        const uint64_t k_at = valid ? (uint64_t)(uint32_t)id * a.k_b + (uint64_t)(uint32_t)off * a.k_l : 0;
-        const uint64_t v_at = (uint64_t)(uint32_t)id * a.v_b + (uint64_t)(uint32_t)off * a.v_l;
-        const char* const k_row = k_head + (k_at << 4);
-        const char* const v_row = valid ? v_head + (v_at << 4) : reinterpret_cast<const char*>(kZeroRow);
-        const uint32_t to = ring + stage * G::kStageBytes + chunk * 1024;
-        to_lds<kOnce>(k_row + R::k_place(row, c) * 16, to);
-        to_lds<kOnce>(v_row + R::v_place(row, c) * 16, to + G::kHalfBytes);
+        const uint2 at = places_at[(step * G::kStep + from_row[i]) & (2 * kWindow - 1)];
+        to_lds<kOnce>(from[i] + ((uint64_t)(from_v[i] ? at.y : at.x) << a.unit), ring + stage * G::kStageBytes + (i * kWaves + wave) * 1024);
       }
     };
-    auto pass = [&](auto safe) {
-      rw.clear();
-      int filled = t0 * G::kStep / kWindow - 1;   // the last window whose page ids are there
+    // Every step in turn: body(step, place of its K in the LDS, next), which has everyone call next() once.
+    auto traverse = [&](auto body) {
+      int placed = t0 * G::kStep / kWindow;       // the last window whose tokens' places are there
       int stage_to = 0, stage_at = 0;
+      if (t0 < t1) {
+        fetch_ids(placed);
+        fetch_ids(placed + 1);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        meet();
+        place_tokens(placed);
+        meet();
+      }
       auto request = [&](int step) {              // (uniform, and so are the barriers in it)
         if (step >= t1) return;
-        if (step * G::kStep / kWindow != filled) fill(++filled);
+        if (step * G::kStep / kWindow != placed) {        // its ids were asked for a window ago, and have landed with the step that everyone has waited for
+          ++placed;
+          place_tokens(placed);
+          meet();
+          fetch_ids(placed + 1);
+        }
         issue(step, stage_to);
         stage_to = stage_to + 1 == G::kStages ? 0 : stage_to + 1;
       };
+      static_assert(kWindow / G::kStep >= G::kStages, "page ids that have landed, places that no one reads any more");
 #pragma clang loop unroll(disable)
       for (int i = 0; i < G::kStages - 1; ++i) request(t0 + i);
 #pragma clang loop unroll(disable)
       for (int t = t0; t < t1; ++t) {
         // all but my youngest requests have landed; after the barrier everyone's have, and everyone is done with the step before
-        static_assert(G::kStages == 2 || G::kStages == 4, "these waits");
-        if (G::kStages == 2 || t + 1 == t1) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        else if (t + 2 == t1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * G::kLoads) : "memory");
-        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(4 * G::kLoads) : "memory");
+        wait_for_all_but<G::kStages - 2, G::kLoads>(t1 - 1 - t);
         meet();
-        request(t + G::kStages - 1);
-        const uint32_t k_lds = ring + stage_at * G::kStageBytes + token_wave * kTile * R::kRowBytes, v_lds = k_lds + G::kHalfBytes;
+        body(t, ring + stage_at * G::kStageBytes, [&] { request(t + G::kStages - 1); });
         stage_at = stage_at + 1 == G::kStages ? 0 : stage_at + 1;
-        if (!works) continue;
-        const int tok0 = t * G::kStep + token_wave * kTile, at = tok0 - base;      // `at`: of the first token among the new ones
-        const int hole = __builtin_amdgcn_readfirstlane(holes[t * G::kStep / kWindow & 1]);
-        if (at <= -kTile && tok0 + kTile <= limit && !hole) {
-          rw.template step<false, decltype(safe)::value>(k_lds + k_lane, v_lds + v_lane, 0u, a.scale_log2e, lane);
-        } else {
-          int off;
-          const int tok = tok0 + (lane & 31), id = page_of(min(tok, limit - 1), &off);
-          const uint32_t live = (uint32_t)__ballot(tok < limit && (unsigned)id < (unsigned)a.pages);
-          uint32_t seen = chain_bits(my_token, at);
-          if (my_mask) {
-            const int w = max(at, 0) >> 6;
-            seen = tree_bits(w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
-          }
-          rw.template step<true, decltype(safe)::value>(k_lds + k_lane, v_lds + v_lane, seen & live, a.scale_log2e, lane);
-        }
       }
       meet();
     };
-    pass(std::false_type{});
-    // A part of a weight may be zero, which times an infinite value is NaN, and so may be the weight of a token that a row does not see.  Nothing else can
-    // come of that: a workgroup whose result holds NaN takes its tokens once more, with two positive numbers for every positive weight and the tokens that some row
-    // does not see one by one.
-    if (tid == 0) *vote = 0;
-    meet();
-    if (works && rw.any_nan() && lane == 0) *vote = 1;
-    meet();
-    if (*vote) pass(std::true_type{});
-
-    // the waves that took other tokens of the same rows together
-    rw.template store<G::kPitch>(part + wave * R::kRows * G::kPitch, lane);
-    const float sum_l = rw.whole_sum();
-    if (R::writes_sum(lane)) part_ml[wave * R::kRows + R::column(lane)] = make_float2(rw.m, sum_l);
-    meet();
-    for (int i = tid; i < unit_rows * (kD / 4); i += kThreads) {
-      const int row = i / (kD / 4), c = i % (kD / 4);
-      const int at = row;                         // row wave row / kRows, column row % kRows: as they are
-      float top = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < G::kTokenWaves; ++w) top = fmaxf(top, part_ml[w * G::kRowTile + at].x);
-      floatx4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < G::kTokenWaves; ++w) {
-        const float2 ml = part_ml[w * G::kRowTile + at];
-        const float f = factor_of(ml.x, top);
-        sum = fmaf(ml.y, f, sum);
-        o += *reinterpret_cast<const floatx4*>(part + (w * G::kRowTile + at) * G::kPitch + 4 * c) * f;
+    auto seen_of = [&](int t) {                   // of the wave's tokens: whether there are any that the lane's row does not see, and which it does
+      const int tok0 = t * G::kStep, at = tok0 - base;         // `at`: of the first token among the new ones
+      constexpr uint32_t kAll = ~0u >> (32 - G::kStep);
+      const uint32_t live = __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t*>(live_at)[(tok0 & (2 * kWindow - 1)) >> 5] >> (tok0 & 31)) & kAll;
+      Seen s{at > -G::kStep || live != kAll, kAll};
+      if (s.masked) {
+        s.bits = chain_bits(my_token, at);
+        if (my_mask) {
+          const int w = max(at, 0) >> 6;
+          s.bits = tree_bits(w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
+        }
+        s.bits &= live;
       }
+      return s;
+    };
+    // Once as it is.  A weight of zero, or a part of one that is, times infinity or NaN is NaN, also where a row does not see the token: if there is NaN in the result
+    // of a workgroup, once more with the values that are finite, and then the others added to the rows that see them.
+    bool clean = false;
+#pragma clang loop unroll(disable)
+    for (;;) {
+      rw.clear();
+      traverse([&](int t, uint32_t k_stage, auto next) {
+        if (clean) {
+          for (int i = tid; i < G::kHalfBytes / 16; i += kThreads) {
+            const lds_chunk_ptr_t at = (lds_chunk_ptr_t)(uintptr_t)(k_stage + G::kHalfBytes + i * 16);
+            *at = R::finite(*at);
+          }
+          meet();
+        }
+        if (!works) {
+          next();
+          return;
+        }
+        rw.step(k_stage + k_lane, k_stage + G::kHalfBytes + v_lane, a.scale_log2e, lane, [&] {
+          const Seen seen = seen_of(t);
+          next();
+          return seen;
+        });
+      });
+      if (clean) break;
+      if (tid == 0) *vote = 0;
+      meet();
+      if (works && rw.any_nan() && lane == 0) *vote = 1;
+      meet();
+      if (!*vote) break;
+      clean = true;
+    }
+    if (clean) {
+      traverse([&](int t, uint32_t k_stage, auto next) {
+        next();
+        if (!works) return;
+        const Seen seen = seen_of(t);
+        const uint32_t on = rw.weighs(k_stage + k_lane, seen, a.scale_log2e, lane);
+#pragma clang loop unroll(disable)
+        for (int i = 0; i < G::kStep; ++i) rw.add_not_finite(k_stage + G::kHalfBytes, i, seen.bits >> i & 1, on >> i & 1, lane);
+      });
+    }
+
+    const float sum = rw.whole_sum();
+    const int row = row_first + R::column(lane);  // of the unit
+    if (row < unit_rows) {
       if (whole) {
-        const int r = unit * G::kRowTile + row, t = (int)a.per_token.div(r), head = kvh * a.group + r - t * a.group;
-        store4<kBf16>(a.out + (seq.row0 + t) * a.out_t + head * a.out_h + c * 4 * kElem, normalised(o, sum));
-        if (a.lse && c == 0) a.lse[(int64_t)(seq.row0 + t) * a.heads_kv * a.group + head] = lse_of(top, sum);
+        char* const to = a.out + (seq.row0 + my_token) * a.out_t + my_head * a.out_h;
+        rw.each(lane, [&](int dim, floatx4 o) { store4<kBf16>(to + dim * kElem, normalised(o, sum)); });
+        if (a.lse && R::writes_sum(lane)) a.lse[(int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head] = lse_of(rw.m, sum);
       } else {
         const int64_t to = (int64_t)place * G::kRowTile + row;
-        *reinterpret_cast<floatx4*>(a.part_o + to * kD + 4 * c) = o;
-        if (c == 0) a.part_ml[to] = make_float2(top, sum);
+        rw.each(lane, [&](int dim, floatx4 o) { *reinterpret_cast<floatx4*>(a.part_o + to * kD + dim) = o; });
+        if (R::writes_sum(lane)) a.part_ml[to] = make_float2(rw.m, sum);
       }
     }
     if constexpr (kSplit) meet();
@@ -679,14 +756,27 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int step, in
   if (a.lse && c == 0) a.lse[id] = lse_of(m, l);
 }
 
-constexpr int kRuns = 512;
-struct Variant { int row_waves, tile, step; };
-// By the rows that a sequence has on average: a wave's rows, twice or four times as many.
+// Waves of a workgroup, rows of its tile, tokens of a step, workgroups that the device holds: by the rows that a sequence has on average.
+struct Variant { int waves, tile, step, runs; };
+template <bool kBf16, int kD, int kWaves>
+constexpr Variant variant() {
+  using G = Geometry<kBf16, kD, kWaves>;
+  return {kWaves, G::kRowTile, G::kStep, 256 * G::kGroups};
+}
+// f(bf16, d, waves) of a call as constants
+template <class F>
+auto with_waves(bool bf16, int d, int waves, F f) {
+  auto pick = [&](auto w) {
+    if (bf16) return d == 128 ? f(std::true_type{}, std::integral_constant<int, 128>{}, w) : f(std::true_type{}, std::integral_constant<int, 64>{}, w);
+    return d == 128 ? f(std::false_type{}, std::integral_constant<int, 128>{}, w) : f(std::false_type{}, std::integral_constant<int, 64>{}, w);
+  };
+  return waves == 2 ? pick(std::integral_constant<int, 2>{}) : waves == 4 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 8>{});
+}
 Variant variant_of(int tokens, int n, int group, int d, bool bf16) {
-  const int wave_rows = bf16 ? 32 : 16, least = !bf16 && d == 128 ? 2 : 1;     // (of whose rows two steps for four waves do not fit the LDS)
-  const int64_t rows = ((int64_t)tokens * group + n - 1) / n;
-  const int row_waves = std::max(rows <= wave_rows ? 1 : rows <= 2 * wave_rows ? 2 : 4, least);
-  return {row_waves, row_waves * wave_rows, kTile * (kWaves / row_waves)};
+  const int64_t wave_rows = bf16 ? 32 : 16, rows = ((int64_t)tokens * group + n - 1) / n;
+  return with_waves(bf16, d, rows <= wave_rows ? 2 : rows <= 3 * wave_rows ? 4 : 8, [](auto b, auto d, auto w) {
+    return variant<decltype(b)::value, decltype(d)::value, decltype(w)::value>();
+  });
 }
 int64_t most_units(int tokens, int n, int heads_kv, int group, int tile) {
   return heads_kv * ((int64_t)tokens * group / tile + std::min(n, tokens));
@@ -706,10 +796,10 @@ TreeWs carve(int n, int64_t runs, int tile, int d) {
   return w;
 }
 
-template <bool kBf16, int kD, int kRowWaves, bool kSplit>
+template <bool kBf16, int kD, int kWaves, bool kSplit>
 basa_status launch_kernel(const TreeArgs& a, hipStream_t st) {
-  using G = Geometry<kBf16, kD, kRowWaves>;
-  const auto kernel = tree_kernel<kBf16, kD, kRowWaves, kSplit, kRowWaves < 4>;
+  using G = Geometry<kBf16, kD, kWaves>;
+  const auto kernel = tree_kernel<kBf16, kD, kWaves, kSplit, true>;
   if (a.n > kPlanBatch) {
     ProfScope prof(K_TREE, st);
     tree_plan_kernel<<<1, 1024, 0, st>>>(a, G::kStep, G::kRowTile, kSplit);
@@ -718,15 +808,15 @@ basa_status launch_kernel(const TreeArgs& a, hipStream_t st) {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, G::kLdsBytes);
   if (e != hipSuccess) return hip_fail(e, "hipFuncSetAttribute(dynamic LDS)");
   ProfScope prof(K_TREE, st);
-  kernel<<<a.groups, kThreads, G::kLdsBytes, st>>>(a);
+  kernel<<<a.groups, G::kThreads, G::kLdsBytes, st>>>(a);
   BASA_HIP_CHECK_LAUNCH("tree_kernel");
   return BASA_OK;
 }
-template <bool kBf16, int kD, int kRowWaves>
+template <bool kBf16, int kD, int kWaves>
 basa_status launch(const TreeArgs& a, bool solo, hipStream_t st) {
-  using G = Geometry<kBf16, kD, kRowWaves>;
-  if (solo) return launch_kernel<kBf16, kD, kRowWaves, false>(a, st);
-  const basa_status s = launch_kernel<kBf16, kD, kRowWaves, true>(a, st);
+  using G = Geometry<kBf16, kD, kWaves>;
+  if (solo) return launch_kernel<kBf16, kD, kWaves, false>(a, st);
+  const basa_status s = launch_kernel<kBf16, kD, kWaves, true>(a, st);
   if (s != BASA_OK) return s;
   ProfScope prof(K_TREE_JOIN, st);
   const int64_t rows = (int64_t)a.tokens * a.heads_kv * a.group;
@@ -746,7 +836,22 @@ size_t tree_workspace_bytes(int tokens, int n, int heads_q, int heads_kv, int d,
   const int group = heads_q / heads_kv;
   const Variant v = variant_of(tokens, n, group, d, bf16);
   if (is_solo(most_units(tokens, n, heads_kv, group, v.tile), row_tokens)) return carve(n, 0, 0, 0).total;
-  return carve(n, std::min<int64_t>(kRuns, most_places(tokens, n, heads_kv, group, v, row_tokens)), v.tile, d).total;
+  return carve(n, std::min<int64_t>(v.runs, most_places(tokens, n, heads_kv, group, v, row_tokens)), v.tile, d).total;
+}
+
+// Tokens' places are 32-bit numbers, in units of the largest power of two up to 256 that divides the strides of pages and tokens, in bytes: 16 at least, and
+// a row in all stores of whole rows.  -1: K or V reaches further than those numbers do.
+int tree_place_unit(const TensorView& k, const TensorView& v) {
+  const int64_t e = k.dtype == BASA_BF16 ? 2 : 4;
+  int unit = 8;
+  for (const TensorView* t : {&k, &v})
+    for (int64_t stride : {t->stride_b, t->stride_l})
+      while ((stride * e) & ((1 << unit) - 1)) --unit;
+  for (const TensorView* t : {&k, &v}) {
+    const double reach = ((double)(t->batch - 1) * t->stride_b + (double)(t->L - 1) * t->stride_l) * e;
+    if (reach >= 4294967295.0 * (1 << unit)) return -1;
+  }
+  return unit;
 }
 
 basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
@@ -759,8 +864,9 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
   a.q = static_cast<const char*>(q.ptr); a.k = static_cast<const char*>(k_pages.ptr); a.v = static_cast<const char*>(v_pages.ptr);
   a.q_t = q.stride_l * e; a.q_h = q.stride_h * e;
   a.k_h = k_pages.stride_h * e; a.v_h = v_pages.stride_h * e;
-  auto chunks = [&](int64_t stride) { return (uint32_t)(stride * e / 16); };
-  a.k_b = chunks(k_pages.stride_b); a.k_l = chunks(k_pages.stride_l); a.v_b = chunks(v_pages.stride_b); a.v_l = chunks(v_pages.stride_l);
+  a.unit = tree_place_unit(k_pages, v_pages);
+  auto in_units = [&](int64_t stride) { return (uint32_t)(stride * e >> a.unit); };
+  a.k_b = in_units(k_pages.stride_b); a.k_l = in_units(k_pages.stride_l); a.v_b = in_units(v_pages.stride_b); a.v_l = in_units(v_pages.stride_l);
   a.table = table; a.table_stride = table_stride; a.lens = lens; a.cu = cu;
   a.n = n; a.tokens = q.L; a.heads_kv = k_pages.heads; a.group = q.heads / k_pages.heads; a.pages = k_pages.batch;
   a.row_tokens = width * k_pages.L;
@@ -771,7 +877,7 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
   const Variant v = variant_of(a.tokens, n, a.group, q.d, bf16);
   const int64_t units = most_units(a.tokens, n, a.heads_kv, a.group, v.tile);
   const bool solo = is_solo(units, a.row_tokens);
-  a.runs = solo ? 0 : (int)std::min<int64_t>(kRuns, most_places(a.tokens, n, a.heads_kv, a.group, v, a.row_tokens));
+  a.runs = solo ? 0 : (int)std::min<int64_t>(v.runs, most_places(a.tokens, n, a.heads_kv, a.group, v, a.row_tokens));
   a.groups = (int)align_up(solo ? units : a.runs, 8);
   const TreeWs w = carve(n, a.runs, v.tile, q.d);
   char* base = static_cast<char*>(ws);
@@ -779,17 +885,9 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
   a.part_o = reinterpret_cast<float*>(base + w.part_o);
   a.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)q.d);
-  auto pick = [&](auto row_waves) {
-    constexpr int W = decltype(row_waves)::value;
-    if (bf16) return q.d == 128 ? launch<true, 128, W>(a, solo, st) : launch<true, 64, W>(a, solo, st);
-    if constexpr (W > 1) {
-      if (q.d == 128) return launch<false, 128, W>(a, solo, st);
-    }
-    return launch<false, 64, W>(a, solo, st);
-  };
-  if (v.row_waves == 1) return pick(std::integral_constant<int, 1>{});
-  if (v.row_waves == 2) return pick(std::integral_constant<int, 2>{});
-  return pick(std::integral_constant<int, 4>{});
+  return with_waves(bf16, q.d, v.waves, [&](auto b, auto d, auto w) {
+    return launch<decltype(b)::value, decltype(d)::value, decltype(w)::value>(a, solo, st);
+  });
 }
 
 }  // namespace basa

@@ -193,6 +193,7 @@ basa_status launch_decode_attn(const TensorView& q, const TensorView& k_pages, c
 
 // Several new tokens of every sequence (attn_tree.hip), and the pages around them (page_ops.hip).
 bool tree_takes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
+int tree_place_unit(const TensorView& k, const TensorView& v);
 size_t tree_workspace_bytes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
 basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                              int64_t table_stride, const int32_t* lens, const int32_t* cu, int n, const int64_t* masks, int words,

@@ -42,7 +42,7 @@ def test_tree_attn(lib):  # noqa: F811
                 dict(strides=(1024, 132)), dict(ws=0x100010)):
         assert _tree(lib, **bad) == INVALID, bad
     for bad in (dict(q=tensor(heads=8, d=96), k=pages(d=96), v=pages(d=96)), dict(q=tensor(heads=8, L=2 ** 21 + 1)), dict(width=2 ** 27, stride=2 ** 27),
-                dict(k=pages(stride_b=2 ** 35)), dict(v=pages(stride_l=2 ** 35, ptr=0x4000000)),
+                dict(k=pages(stride_b=2 ** 37)), dict(v=pages(stride_l=2 ** 40, ptr=0x4000000)), dict(k=pages(stride_b=2 ** 32 + 8)),
                 dict(q=tensor(heads=8, L=200000), width=2 ** 26, stride=2 ** 26)):
         assert _tree(lib, **bad) == UNSUPPORTED, bad
     for bad in (dict(ws=None), dict(ws_bytes=0), dict(ws_bytes=lib.basa_tree_workspace_size(C.byref(good), C.byref(pages()), C.byref(pages()), 4, 10) - 1)):
