@@ -435,6 +435,7 @@ basa_status basa_cache_copy(const basa_tensor* k_pages, const basa_tensor* v_pag
  * The pages that no sequence holds: those of 0 .. n_pages - 1 that are not among the first ceil(lens[i] / page) entries of any row, ascending.  A page that several hold is
  * free when the last of them ends; a sequence that ends, or is cut back, gets its new length and nothing else.  (Whatever else has to be
  * kept has a row: a prefix that stays for later prompts, say.)
+ *   n_seq up to 2^22, n_pages up to 2^26.
  *   free_pages   out [n_pages] int32: the free ones come first, the rest is left as it was.   count: out [1] int32, how many.
  *   ws           workspace of basa_page_free_workspace_size() bytes.  Nothing in it has to start at zero.
  * No output may overlap an input or another output.

@@ -352,7 +352,7 @@ basa_status check_varlen(const basa_tensor* q, const basa_tensor* k, const basa_
 
 // ---- paged key-value cache ------------------------------------------------------------------
 // Largest counts that the kernels take as 32-bit numbers with room for a step beyond them.
-constexpr int kMaxPagedTokens = 1 << 30, kMaxDecodeRows = 1 << 22, kMaxTreeRows = 1 << 24;
+constexpr int kMaxPagedTokens = 1 << 30, kMaxDecodeRows = 1 << 22, kMaxTreeRows = 1 << 24, kMaxPages = 1 << 26;
 
 basa_status check_pages(const basa_tensor* k, const basa_tensor* v) {
   basa_status s;
@@ -962,7 +962,7 @@ namespace {
 basa_status check_free(int32_t n_seq, int32_t width, int32_t n_pages) {
   if (n_seq < 0 || width < 1) { set_error("a block table of %d rows, %d wide", n_seq, width); return BASA_ERR_INVALID_ARG; }
   if (n_pages < 1) { set_error("a cache has pages (got %d)", n_pages); return BASA_ERR_INVALID_ARG; }
-  if (n_pages > kMaxPagedTokens || n_seq > kMaxDecodeRows) { set_error("%d pages, %d sequences: more than a call takes", n_pages, n_seq); return BASA_ERR_UNSUPPORTED; }
+  if (n_pages > kMaxPages || n_seq > kMaxDecodeRows) { set_error("%d pages, %d sequences: more than a call takes", n_pages, n_seq); return BASA_ERR_UNSUPPORTED; }
   return BASA_OK;
 }
 }  // namespace

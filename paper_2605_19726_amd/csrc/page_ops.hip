@@ -63,60 +63,148 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* parents,
 }
 
 // ---- kept tokens moved together --------------------------------------------------------------------
-// Token start + keep[j] of a sequence to start + j, in place.  keep ascends, so keep[j] >= j: no move writes what a later one reads, and each
-// has to read before the one that writes there, which is a later one or itself.  So a lane that has the same 16 bytes of every row, and moves them in
-// order, needs no one else.
+// Token start + keep[j] of a sequence to start + j, in place.  keep ascends, so keep[j] >= j: no move writes what a later one reads, and what one reads is written by
+// a later one or itself.  So whoever moves the same bytes of every row needs no one else, if of any two rows it reads the first before it writes the second: a lane in the
+// order of the list, or a workgroup that reads many rows before it writes them.
 struct CompactArgs {
   char *k, *v;
   int64_t k_b, k_h, k_l, v_b, v_h, v_l;     // bytes
   const int32_t *table, *start, *keep, *count;
   int64_t table_stride, keep_stride;
-  int width, most, pages, chunk_bits, chunks;          // 16-byte chunks of one token: heads << chunk_bits
+  int width, most, pages, row_bits, parts;  // bytes of a row of one head; parts of K and V of a token: of a lane or a workgroup
   FastDiv page;
 };
+// Where move j of a sequence reads and writes in K or V, from the head's row on; -1: no move.
+struct Move { int64_t from, to; };
+__device__ __forceinline__ Move move_of(const CompactArgs& a, int seq, int start, int j, int64_t page_bytes, int64_t row_bytes) {
+  const int64_t room = (int64_t)a.width * a.page.d;
+  const int kept = a.keep[(int64_t)seq * a.keep_stride + j];
+  const int32_t* const row = a.table + (int64_t)seq * a.table_stride;
+  const int64_t from = (int64_t)start + kept, to = (int64_t)start + j;
+  if (start < 0 || kept <= j || from >= room) return {-1, -1};
+  const int from_page = (int)a.page.div((uint32_t)from), to_page = (int)a.page.div((uint32_t)to);
+  const int from_id = row[from_page], to_id = row[to_page];
+  if ((unsigned)from_id >= (unsigned)a.pages || (unsigned)to_id >= (unsigned)a.pages) return {-1, -1};
+  return {from_id * page_bytes + (from - (int64_t)from_page * a.page.d) * row_bytes, to_id * page_bytes + (to - (int64_t)to_page * a.page.d) * row_bytes};
+}
+
+// Short lists, the paths of trees: a lane to every 16 bytes of a token.  Bound by latency.
 constexpr int kMoves = 256, kAtOnce = 8;
 __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
-  __shared__ int64_t from_at[2][kMoves], to_at[2][kMoves];          // K, V; negative: no move
-  const int seq = blockIdx.x, tid = threadIdx.x, chunk = blockIdx.y * 256 + tid;
+  __shared__ Move moves[2][kMoves];         // K, V
+  const int seq = blockIdx.x, tid = threadIdx.x, part = blockIdx.y * 256 + tid;
   const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq];
-  const bool is_v = chunk >= a.chunks;
-  const int c = is_v ? chunk - a.chunks : chunk;
-  const int64_t h = c >> a.chunk_bits, in_row = (c & ((1 << a.chunk_bits) - 1)) * 16;
+  const bool is_v = part >= a.parts;
+  const int c = is_v ? part - a.parts : part;
+  const int64_t h = c >> (a.row_bits - 4), in_row = (c & ((1 << (a.row_bits - 4)) - 1)) * 16;
   char* const rows = (is_v ? a.v + h * a.v_h : a.k + h * a.k_h) + in_row;
-  const bool works = chunk < 2 * a.chunks;
-  const int64_t room = (int64_t)a.width * a.page.d;
-  auto page_of = [&](int64_t tok, int* off) {
-    if (tok < 0 || tok >= room) return -1;
-    const int p = (int)a.page.div((uint32_t)tok);
-    *off = (int)tok - p * (int)a.page.d;
-    return a.table[(int64_t)seq * a.table_stride + p];
-  };
+  const bool works = part < 2 * a.parts;
   for (int j0 = 0; j0 < count; j0 += kMoves) {
     const int n = min(count - j0, kMoves);
     if (tid < n) {
-      const int j = j0 + tid, kept = a.keep[(int64_t)seq * a.keep_stride + j];
-      int from_off = 0, to_off = 0;
-      const int from = page_of((int64_t)start + kept, &from_off), to = page_of((int64_t)start + j, &to_off);
-      const bool moves = start >= 0 && kept > j && (unsigned)from < (unsigned)a.pages && (unsigned)to < (unsigned)a.pages;
-      from_at[0][tid] = moves ? from * a.k_b + from_off * a.k_l : -1;
-      from_at[1][tid] = moves ? from * a.v_b + from_off * a.v_l : -1;
-      to_at[0][tid] = moves ? to * a.k_b + to_off * a.k_l : -1;
-      to_at[1][tid] = moves ? to * a.v_b + to_off * a.v_l : -1;
+      moves[0][tid] = move_of(a, seq, start, j0 + tid, a.k_b, a.k_l);
+      moves[1][tid] = move_of(a, seq, start, j0 + tid, a.v_b, a.v_l);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __syncthreads();
     for (int i0 = 0; works && i0 < n; i0 += kAtOnce) {
       uintx4 x[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) x[i] = *reinterpret_cast<const uintx4*>(rows + max(from_at[is_v][min(i0 + i, n - 1)], (int64_t)0));
+      for (int i = 0; i < kAtOnce; ++i) x[i] = *reinterpret_cast<const uintx4*>(rows + max(moves[is_v][min(i0 + i, n - 1)].from, (int64_t)0));
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i)
-        if (i0 + i < n && to_at[is_v][i0 + i] >= 0) *reinterpret_cast<uintx4*>(rows + to_at[is_v][i0 + i]) = x[i];
+        if (i0 + i < n && moves[is_v][i0 + i].to >= 0) *reinterpret_cast<uintx4*>(rows + moves[is_v][i0 + i].to) = x[i];
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __syncthreads();
   }
 }
+
+// Long lists: a workgroup to every 128 bytes of a token's K or V, eight lanes to a row, eight rows to each of them read before one is written, a move to every thread.  The
+// next rows are read while these are written; what their places come from was asked for a turn and two turns earlier.  Bound by the memory, or by the longest list, whose
+// workgroups take turn after turn.
+constexpr int kLine = 128, kLinesAtOnce = 8;
+template <int kThreads>
+__global__ __launch_bounds__(kThreads, 4) void compact_lines_kernel(CompactArgs a) {
+  __shared__ Move moves[3][kThreads];         // of the rows that are written, of those that are read, of the next
+  const int seq = blockIdx.x / (2 * a.parts), part = blockIdx.x - seq * 2 * a.parts, tid = threadIdx.x;
+  const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq];
+  if (count == 0) return;
+  const bool is_v = part >= a.parts;
+  const int c = is_v ? part - a.parts : part;
+  const int64_t h = c >> (a.row_bits - 7), in_row = (c & ((1 << (a.row_bits - 7)) - 1)) * kLine + (tid & 7) * 16;
+  char* const rows = (is_v ? a.v + h * a.v_h : a.k + h * a.k_h) + in_row;
+  const int64_t page_bytes = is_v ? a.v_b : a.k_b, row_bytes = is_v ? a.v_l : a.k_l, room = (int64_t)a.width * a.page.d;
+  const int32_t* const keep = a.keep + (int64_t)seq * a.keep_stride;
+  const int32_t* const table = a.table + (int64_t)seq * a.table_stride;
+  // A thread's move of the turn that begins with j0, in three steps: the kept token, the ids of its pages, its place.  (No branches, so that nothing waits within one.)
+  struct Kept { int j, token; };
+  struct Pages { int64_t from, to; int from_page, to_page, from_id, to_id; bool valid; };
+  auto ask_token = [&](int j0) {
+    const int j = j0 + tid;
+    return Kept{j, keep[min(j, count - 1)]};
+  };
+  auto ask_pages = [&](Kept k) {
+    Pages p;
+    p.from = (int64_t)start + k.token;
+    p.to = (int64_t)start + k.j;
+    p.valid = k.j < count && start >= 0 && k.token > k.j && p.from < room;
+    p.from_page = (int)a.page.div(p.valid ? (uint32_t)p.from : 0u);
+    p.to_page = (int)a.page.div(p.valid ? (uint32_t)p.to : 0u);
+    p.from_id = table[p.from_page];
+    p.to_id = table[p.to_page];
+    return p;
+  };
+  auto put_move = [&](Pages p, int side) {
+    const bool valid = p.valid && (unsigned)p.from_id < (unsigned)a.pages && (unsigned)p.to_id < (unsigned)a.pages;
+    moves[side][tid] = valid ? Move{p.from_id * page_bytes + (p.from - (int64_t)p.from_page * a.page.d) * row_bytes,
+                                    p.to_id * page_bytes + (p.to - (int64_t)p.to_page * a.page.d) * row_bytes} : Move{-1, -1};
+  };
+  auto read = [&](uintx4 (&x)[kLinesAtOnce], int side) {
+#pragma unroll
+    for (int i = 0; i < kLinesAtOnce; ++i) x[i] = *reinterpret_cast<const uintx4*>(rows + max(moves[side][i * (kThreads / 8) + (tid >> 3)].from, (int64_t)0));
+  };
+  auto write = [&](const uintx4 (&x)[kLinesAtOnce], int side) {
+#pragma unroll
+    for (int i = 0; i < kLinesAtOnce; ++i) {
+      const int64_t to = moves[side][i * (kThreads / 8) + (tid >> 3)].to;
+      if (to >= 0) *reinterpret_cast<uintx4*>(rows + to) = x[i];
+    }
+  };
+  // vmcnt(0) lgkmcnt(0): my rows are here, and my move is in the LDS; after the barrier everyone's
+  auto meet = [&] {
+    __builtin_amdgcn_s_waitcnt(0x0070);
+    asm volatile("" ::: "memory");
+    __syncthreads();
+  };
+  uintx4 x[kLinesAtOnce], y[kLinesAtOnce];
+  int side = 0;
+  auto next = [&](int at) { return at == 2 ? 0 : at + 1; };
+  Kept kept = ask_token(0);
+  Pages pages = ask_pages(kept);
+  kept = ask_token(kThreads);
+  put_move(pages, 0);
+  pages = ask_pages(kept);
+  kept = ask_token(2 * kThreads);
+  meet();
+  read(x, 0);
+  // The rows before j0 are in `mine` or on their way there; those from j0 on go to `others`.  False: there are none.
+  auto turn = [&](uintx4 (&mine)[kLinesAtOnce], uintx4 (&others)[kLinesAtOnce], int j0) {
+    const int ahead = next(side);
+    put_move(pages, ahead);
+    meet();
+    pages = ask_pages(kept);                    // of j0 + kThreads
+    kept = ask_token(j0 + 2 * kThreads);
+    if (j0 < count) read(others, ahead);
+    write(mine, side);
+    side = ahead;
+    return j0 < count;
+  };
+  for (int j0 = kThreads; turn(x, y, j0) && turn(y, x, j0 + kThreads); j0 += 2 * kThreads) {
+  }
+}
+// Up to this many moves a list is short.
+constexpr int kShortList = 64;
 
 // ---- sequences that go on from others --------------------------------------------------------------
 // New sequence j shares the whole pages of its parent.  The page that is not full, if there is one, goes to the first new sequence of the parent; each
@@ -225,38 +313,51 @@ struct FreeArgs {
   int64_t table_stride;
   int n, row_tokens, pages, words;          // words of 32 bits
   int32_t *free_pages, *count;
-  uint32_t* used;                           // workspace
+  uint8_t* used;                            // workspace: a byte for every page, up to a multiple of 32
   FastDiv page;
 };
-// Marks the pages of the row of a wave.
-template <class Mark>
-__device__ __forceinline__ void mark_row(const FreeArgs& a, int i, Mark mark) {
-  const int held = pages_of(a.page, min(max(a.lens[i], 0), a.row_tokens));
-  const int32_t* const row = a.table + (int64_t)i * a.table_stride;
-  for (int p = threadIdx.x & 63; p < held; p += 64) {
-    const int id = row[p];
-    if ((unsigned)id < (unsigned)a.pages) mark(id);
+// Marks the pages of kRows rows, `apart` entries one behind the other, by a wave: 8 / kRows entries of each to a lane asked for at once.
+template <int kRows, class Mark>
+__device__ __forceinline__ void mark_rows(const FreeArgs& a, const int32_t* row, int64_t apart, const int (&held)[kRows], Mark mark) {
+  constexpr int kEntries = 8 / kRows;
+  int most = held[0];
+#pragma unroll
+  for (int r = 1; r < kRows; ++r) most = max(most, held[r]);
+  for (int p0 = threadIdx.x & 63; p0 < most + 63; p0 += 64 * kEntries) {         // (as many turns for every lane)
+    int id[kRows][kEntries];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int i = 0; i < kEntries; ++i) id[r][i] = p0 + 64 * i < held[r] ? row[r * apart + p0 + 64 * i] : -1;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int i = 0; i < kEntries; ++i)
+        if ((unsigned)id[r][i] < (unsigned)a.pages) mark(id[r][i]);
   }
 }
-// The free pages of words [first, first + n) of `used` (the last word's bits past the end are set), by the whole workgroup, from place `at` of the list on.
+__device__ __forceinline__ int held_pages(const FreeArgs& a, int i) { return pages_of(a.page, min(max(a.lens[i], 0), a.row_tokens)); }
+// The free pages of words [first, first + n), which are in the LDS (the last word's bits past the end are set), by the whole workgroup, from place `at` of the list on.  Returns
+// the place behind them.
 template <int kThreads>
 __device__ __forceinline__ int list_free(const FreeArgs& a, const uint32_t* used, int first, int n, int at, int* wave_sum) {
   constexpr int kGroupWaves = kThreads / 64;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int each = (n + kGroupWaves - 1) / kGroupWaves, w0 = min(wave * each, n), w1 = min(w0 + each, n);       // words of a wave
   int mine = 0;
-  for (int w = w0 + lane; w < w1; w += 64) mine += __popc(~used[first + w]);
+  for (int w = w0 + lane; w < w1; w += 64) mine += __popc(~used[w]);
   const int sum = __builtin_amdgcn_readlane((int)wave_scan((uint32_t)mine, sum_of), 63);
   if (lane == 0) wave_sum[wave] = sum;
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   int all = at;
+#pragma unroll
   for (int w = 0; w < kGroupWaves; ++w) {
     if (w < wave) at += wave_sum[w];
     all += wave_sum[w];
   }
   for (int w = w0; w < w1; w += 2) {           // 64 pages at a time
-    const bool free = w + (lane >> 5) < w1 && !(used[first + min(w + (lane >> 5), w1 - 1)] >> (lane & 31) & 1);
+    const bool free = w + (lane >> 5) < w1 && !(used[min(w + (lane >> 5), w1 - 1)] >> (lane & 31) & 1);
     const uint64_t which = __ballot(free);
     if (free) a.free_pages[at + __popcll(which & ((1ull << lane) - 1))] = (first + w) * 32 + lane;
     at += __popcll(which);
@@ -270,35 +371,69 @@ __device__ __forceinline__ uint32_t past_the_end(const FreeArgs& a, int word) {
 __global__ __launch_bounds__(1024) void page_free_kernel(FreeArgs a) {
   extern __shared__ uint32_t used[];
   __shared__ int wave_sum[16];
+  const int wave = threadIdx.x >> 6;
   for (int w = threadIdx.x; w < a.words; w += 1024) used[w] = past_the_end(a, w);
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
-  for (int i = threadIdx.x >> 6; i < a.n; i += 16) mark_row(a, i, [&](int id) { atomicOr(&used[id >> 5], 1u << (id & 31)); });
+  for (int i0 = wave; i0 < a.n; i0 += 1024) {                 // every 16th row to a wave: 64 lengths at once, four rows at a time
+    const int i = i0 + 16 * (threadIdx.x & 63), mine = i < a.n ? held_pages(a, i) : 0;
+    for (int r = 0; r < 64 && i0 + 16 * r < a.n; r += 4) {
+      const int held[4] = {__builtin_amdgcn_readlane(mine, r), __builtin_amdgcn_readlane(mine, r + 1), __builtin_amdgcn_readlane(mine, r + 2),
+                           __builtin_amdgcn_readlane(mine, r + 3)};
+      mark_rows(a, a.table + (int64_t)(i0 + 16 * r) * a.table_stride, 16 * a.table_stride, held, [&](int id) { atomicOr(&used[id >> 5], 1u << (id & 31)); });
+    }
+  }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   const int all = list_free<1024>(a, used, 0, a.words, 0, wave_sum);
   if (threadIdx.x == 0) *a.count = all;
 }
+// Over the device a byte for every page: stores of ones need no order, and atomics on bits, which go past the XCDs' caches, took 18 of 26 us of a call of 2000 rows.
 __global__ __launch_bounds__(256) void free_clear_kernel(FreeArgs a) {
-  const int w = blockIdx.x * 256 + threadIdx.x;
-  if (w < a.words) a.used[w] = past_the_end(a, w);
+  const int p0 = (blockIdx.x * 256 + threadIdx.x) * 16;
+  if (p0 >= a.words * 32) return;
+  uintx4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int left = a.pages - p0 - 4 * i;      // (the bytes past the last page are ones)
+    x[i] = left >= 4 ? 0u : left <= 0 ? 0x01010101u : 0x01010101u << (8 * left);
+  }
+  *reinterpret_cast<uintx4*>(a.used + p0) = x;
 }
 __global__ __launch_bounds__(256) void free_mark_kernel(FreeArgs a) {
   const int i = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i < a.n) mark_row(a, i, [&](int id) { atomicOr(&a.used[id >> 5], 1u << (id & 31)); });
+  if (i >= a.n) return;
+  const int held[1] = {held_pages(a, i)};
+  mark_rows(a, a.table + (int64_t)i * a.table_stride, 0, held, [&](int id) { a.used[id] = 1; });
 }
+// A workgroup counts the free pages before its words for itself.
+constexpr int kListWords = 2048;
 __global__ __launch_bounds__(1024) void free_list_kernel(FreeArgs a, int words_each) {
   __shared__ int before[16], wave_sum[16];
+  __shared__ uint32_t used[kListWords];
   const int first = blockIdx.x * words_each, n = min(words_each, a.words - first), tid = threadIdx.x;
   int mine = 0;
-  for (int w = tid; w < first; w += 1024) mine += __popc(~a.used[w]);
+  const uintx4* const bytes = reinterpret_cast<const uintx4*>(a.used);
+  constexpr int kLoads = 4;
+  for (int c0 = 0; c0 < 2 * first; c0 += 1024 * kLoads) {     // 16 pages each
+    uintx4 x[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) x[i] = bytes[min(c0 + 1024 * i + tid, 2 * a.words - 1)];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) mine += c0 + 1024 * i + tid < 2 * first ? 16 - __popc(x[i][0]) - __popc(x[i][1]) - __popc(x[i][2]) - __popc(x[i][3]) : 0;
+  }
+  for (int w = (tid >> 6) * 2; w < n; w += 32) {              // 64 pages at a time as bits
+    const uint64_t bits = __ballot(w + (tid >> 5 & 1) < n && a.used[(int64_t)(first + min(w + (tid >> 5 & 1), n - 1)) * 32 + (tid & 31)]);
+    if ((tid & 31) == 0 && w + (tid >> 5 & 1) < n) used[w + (tid >> 5 & 1)] = (uint32_t)(tid & 32 ? bits >> 32 : bits);
+  }
   const int sum = __builtin_amdgcn_readlane((int)wave_scan((uint32_t)mine, sum_of), 63);
   if ((tid & 63) == 0) before[tid >> 6] = sum;
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
   int at = 0;
+#pragma unroll
   for (int w = 0; w < 16; ++w) at += before[w];
-  const int all = list_free<1024>(a, a.used, first, n, at, wave_sum);
+  const int all = list_free<1024>(a, used, first, n, at, wave_sum);
   if (first + n == a.words && tid == 0) *a.count = all;
 }
 // In one workgroup, or in three launches over the device.
@@ -326,12 +461,20 @@ basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_
   a.v_b = v_pages.stride_b * e; a.v_h = v_pages.stride_h * e; a.v_l = v_pages.stride_l * e;
   a.table = table; a.start = start; a.keep = keep; a.count = count; a.table_stride = table_stride; a.keep_stride = keep_stride;
   a.width = width; a.most = most; a.pages = k_pages.batch;
-  while ((16 << a.chunk_bits) < k_pages.d * e) ++a.chunk_bits;
-  a.chunks = k_pages.heads << a.chunk_bits;
+  while ((1 << a.row_bits) < k_pages.d * e) ++a.row_bits;
   a.page = fast_div((uint32_t)k_pages.L);
   ProfScope prof(K_PAGED, st);
-  compact_kernel<<<dim3(n, ceil_div(2 * a.chunks, 256)), 256, 0, st>>>(a);
-  BASA_HIP_CHECK_LAUNCH("compact_kernel");
+  if (most <= kShortList) {
+    a.parts = k_pages.heads << (a.row_bits - 4);
+    compact_kernel<<<dim3(n, ceil_div(2 * a.parts, 256)), 256, 0, st>>>(a);
+    BASA_HIP_CHECK_LAUNCH("compact_kernel");
+  } else {
+    a.parts = k_pages.heads << (a.row_bits - 7);
+    const unsigned groups = (unsigned)n * 2 * a.parts;
+    if (groups >= 512) compact_lines_kernel<512><<<groups, 512, 0, st>>>(a);
+    else compact_lines_kernel<1024><<<groups, 1024, 0, st>>>(a);
+    BASA_HIP_CHECK_LAUNCH("compact_lines_kernel");
+  }
   return BASA_OK;
 }
 
@@ -373,13 +516,13 @@ basa_status launch_cache_copy(const TensorView& k_pages, const TensorView& v_pag
 }
 
 size_t page_free_workspace_bytes(int n_seq, int width, int n_pages) {
-  return free_in_one(n_seq, width, n_pages) ? 256 : align_up((size_t)ceil_div(n_pages, 32) * 4, 256);
+  return free_in_one(n_seq, width, n_pages) ? 256 : align_up((size_t)ceil_div(n_pages, 32) * 32, 256);
 }
 basa_status launch_page_free(const int32_t* table, int width, int64_t table_stride, const int32_t* lens, int n_seq, int page, int n_pages,
                              int32_t* free_pages, int32_t* count, void* ws, hipStream_t st) {
   FreeArgs a{};
   a.table = table; a.lens = lens; a.table_stride = table_stride; a.n = n_seq; a.row_tokens = width * page; a.pages = n_pages;
-  a.words = ceil_div(n_pages, 32); a.free_pages = free_pages; a.count = count; a.used = static_cast<uint32_t*>(ws);
+  a.words = ceil_div(n_pages, 32); a.free_pages = free_pages; a.count = count; a.used = static_cast<uint8_t*>(ws);
   a.page = fast_div((uint32_t)page);
   ProfScope prof(K_PAGED, st);
   if (free_in_one(n_seq, width, n_pages)) {
@@ -387,13 +530,13 @@ basa_status launch_page_free(const int32_t* table, int width, int64_t table_stri
     BASA_HIP_CHECK_LAUNCH("page_free_kernel");
     return BASA_OK;
   }
-  free_clear_kernel<<<ceil_div(a.words, 256), 256, 0, st>>>(a);
+  free_clear_kernel<<<ceil_div(2 * a.words, 256), 256, 0, st>>>(a);
   BASA_HIP_CHECK_LAUNCH("free_clear_kernel");
   if (n_seq > 0) {
     free_mark_kernel<<<ceil_div(n_seq, 4), 256, 0, st>>>(a);
     BASA_HIP_CHECK_LAUNCH("free_mark_kernel");
   }
-  const int groups = std::min(ceil_div(a.words, 64), 64), each = ceil_div(a.words, groups);
+  const int groups = std::max(std::min(ceil_div(a.words, 64), 128), ceil_div(a.words, kListWords)), each = ceil_div(a.words, groups);
   free_list_kernel<<<ceil_div(a.words, each), 1024, 0, st>>>(a, each);
   BASA_HIP_CHECK_LAUNCH("free_list_kernel");
   return BASA_OK;

@@ -105,9 +105,9 @@ def test_page_free(lib):  # noqa: F811
                 dict(ws=0x100010), dict(free=0x10000), dict(free=0x1000 - 1196), dict(count=0x1000 + 36), dict(count=0x2000 + 1196), dict(ws=0x10000),
                 dict(ws=0x2000)):
         assert call(**bad) == INVALID, bad
-    for bad in (dict(ws=None), dict(ws_bytes=255), dict(pages=2 ** 20, free=2 ** 40, ws_bytes=2 ** 17 - 1)):
+    for bad in (dict(ws=None), dict(ws_bytes=255), dict(pages=2 ** 20, free=2 ** 40, ws_bytes=2 ** 20 - 1)):
         assert call(**bad) == WORKSPACE, bad
-    for bad in (dict(pages=2 ** 30 + 1, free=2 ** 40), dict(width=2 ** 27, stride=2 ** 27)):
+    for bad in (dict(pages=2 ** 26 + 1, free=2 ** 40), dict(n=2 ** 22 + 1, table=2 ** 50, lens=2 ** 45), dict(width=2 ** 27, stride=2 ** 27)):
         assert call(**bad) == UNSUPPORTED, bad
     assert lib.basa_page_free_workspace_size(10, 20, 0) == 0 and lib.basa_page_free_workspace_size(0, 20, 2 ** 20) >= 2 ** 17
 
