@@ -42,7 +42,8 @@ struct TreeArgs {
   float* lse;                               // [tokens][heads_q] or null
   int groups;                               // workgroups, a multiple of 8
   int runs;                                 // at most so many runs (cut by runs)
-  int* first_place;                         // workspace: [n + 1] first place of every sequence, then how many there are
+  int* first_place;                         // workspace, of more than kPlanBatch sequences: [n + 1] first place of each for one head, then how many there are
+  int* cut_of;                              // workspace: [tokens][heads_q] first and last run that have steps of a row, and its place in the tile; -1: one run has all
   float* part_o;                            // [2 runs][tile][d], not normalised
   float2* part_ml;                          // [2 runs][tile] maximum in units of the exponent, sum
   float scale_log2e;                        // log2 e / sqrt(d)
@@ -61,6 +62,8 @@ __device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
   s.n = max(min(a.cu[b + 1], a.tokens) - s.row0, 0);
   return s;
 }
+constexpr int kMostRuns = 1024, kMostRows = 256;
+__device__ __forceinline__ int pack_cut(int first, int last, int row) { return first + kMostRuns * (last + kMostRuns * row); }
 __device__ __forceinline__ int sum_of(int x, int y) { return x + y; }
 template <int kOff>
 __device__ __forceinline__ float pair_max(float v) {
@@ -285,6 +288,26 @@ struct Rows<true, kD> {
 #pragma unroll
       for (int i = 0; i < 16; i += 4) f(32 * e + 2 * i + 4 * (lane >> 5), floatx4{acc[e][i], acc[e][i + 1], acc[e][i + 2], acc[e][i + 3]});
   }
+  // The row divided by its sum: lanes h and 32 + h have four dimensions each of the same eight, and exchange them for eight each of sixteen.
+  __device__ __forceinline__ void store(char* to, float sum, int lane, bool mine) const {
+    const float by = 1.0f / sum;
+    const auto part = [&](float o) { return (__bf16)(sum == 0.f ? 0.f : o * by); };
+#pragma unroll
+    for (int e = 0; e < kBlocks; ++e)
+#pragma unroll
+      for (int i = 0; i < 16; i += 8) {
+        uintx4 t;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+          const auto pair = [&](int at) { return __builtin_bit_cast(uint32_t, bf16x2{part(acc[e][at]), part(acc[e][at + 1])}); };
+          const auto both = __builtin_amdgcn_permlane32_swap(pair(i + 2 * j), pair(i + 4 + 2 * j), false, false);
+          t[j] = both[0];
+          t[2 + j] = both[1];
+        }
+        if (mine) *reinterpret_cast<uintx4*>(to + (32 * e + 2 * i + 8 * (lane >> 5)) * 2) = t;
+      }
+  }
 };
 
 // f32: 16 rows, 16x16x4 instructions, 16 tokens.  S^T = K Q^T: lane (g, r) holds chunk 4 c + g of token r, four products; the score is the sum of four sums of d / 4.
@@ -418,19 +441,23 @@ struct Rows<false, kD> {
       for (int x = 0; x < kD / 64; ++x)
         f(64 * x + 4 * (4 * (lane >> 4) + i), floatx4{acc[4 * x][i], acc[4 * x + 1][i], acc[4 * x + 2][i], acc[4 * x + 3][i]});
   }
+  __device__ __forceinline__ void store(char* to, float sum, int lane, bool mine) const {
+    each(lane, [&](int dim, floatx4 o) { if (mine) *reinterpret_cast<floatx4*>(to + dim * 4) = normalised(o, sum); });
+  }
 };
 
 // A workgroup has a wave for every kRows rows of a tile; each takes every token.  Of a ring of kStages steps in the LDS one is worked on, the others are on
-// their way there.
-template <bool kBf16, int kD, int kWaves>
+// their way there: 64 KB for a workgroup of two or four waves, two to a compute unit, 128 KB for one of eight.  Short sequences of few rows want more workgroups, not more
+// steps ahead: two steps in the ring and four workgroups (64 sequences of 60 tokens, bf16, d = 128: 16.4 -> 12.1 us; 512 of them 110 -> 87).
+template <bool kBf16, int kD, int kWaves, bool kSplit>
 struct Geometry {
   using R = Rows<kBf16, kD>;
   static constexpr int kThreads = 64 * kWaves, kStep = R::kTokens, kRowTile = R::kRows * kWaves;
   static constexpr int kHalfBytes = kStep * R::kRowBytes, kStageBytes = 2 * kHalfBytes;      // K, then V: 8 or 16 KB
   static constexpr int kLoads = kStageBytes / 1024 / kWaves;                                 // of a wave for a step, 1 KB each
   static constexpr bool kLarge = kStageBytes > 8 * 1024;
-  static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? (kLarge ? 4 : 8) : 4;
-  static constexpr int kGroups = kWaves == 8 ? 1 : kWaves == 4 ? 2 : kLarge ? 2 : 4;         // workgroups that a compute unit holds
+  static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? (kLarge ? 4 : 8) : kLarge && !kSplit ? 2 : 4;
+  static constexpr int kGroups = kWaves == 8 ? 1 : kWaves == 4 ? 2 : kLarge && kSplit ? 2 : 4;         // workgroups that a compute unit holds
   static constexpr int kWavesPerSimd = (kGroups * kWaves + 3) / 4;
   static constexpr int kPlacesAt = kStages * kStageBytes, kIdsAt = kPlacesAt + 2 * kWindow * 8;       // places of K and V, page ids
   static constexpr int kLiveAt = kIdsAt + 2 * kWindow * 4, kVoteAt = kLiveAt + 2 * kWindow / 8, kLdsBytes = kVoteAt + 16;
@@ -445,10 +472,10 @@ __device__ __forceinline__ void wait_for_all_but(int steps) {
 }
 
 template <bool kBf16, int kD, int kWaves, bool kSplit, bool kOnce>
-__global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPerSimd)) void tree_kernel(TreeArgs a) {
-  using G = Geometry<kBf16, kD, kWaves>;
+__global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::kWavesPerSimd)) void tree_kernel(TreeArgs a) {
+  using G = Geometry<kBf16, kD, kWaves, kSplit>;
   using R = Rows<kBf16, kD>;
-  constexpr int kElem = kBf16 ? 2 : 4, kLead = kSplit ? tree_lead(G::kStep) : 0, kThreads = G::kThreads;
+  constexpr int kLead = kSplit ? tree_lead(G::kStep) : 0, kThreads = G::kThreads;
   extern __shared__ __attribute__((aligned(1024))) char smem[];
   int* const ids = reinterpret_cast<int*>(smem + G::kIdsAt);
   uint2* const places_at = reinterpret_cast<uint2*>(smem + G::kPlacesAt);
@@ -458,65 +485,82 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
   auto places_of = [&](const Sequence& s) {       // of one unit
     return kSplit ? tree_steps(s.len, G::kStep) + kLead : 1;
   };
-  auto all_places = [&](const Sequence& s) { return tree_units(s.n * a.group, G::kRowTile) * places_of(s) * a.heads_kv; };
+  auto all_places = [&](const Sequence& s) { return tree_units(s.n * a.group, G::kRowTile) * places_of(s); };
 
-  // the run of this workgroup and the sequence that its first place is of.  Neighbours on the axis run on one XCD
+  // The run of this workgroup, and the head and sequence that its first place is of.  Neighbours on the axis run on one XCD: a KV head, or several, where there are eight or more.
   const int group = (blockIdx.x & 7) * (a.groups >> 3) + (blockIdx.x >> 3);
-  int b = 0, first = 0, total, run = 1;
+  int b = 0, first = 0, of_head, run = 1, kvh = 0;        // of_head: places of a head; first: of the sequence, among them all
+  Sequence mine_of{};                             // of n <= 64: that of the lane's sequence
   if (a.n <= kPlanBatch) {                        // a few sequences to a lane
     const int each = (a.n + 63) / 64;
     int mine = 0;
-    for (int i = 0; i < each; ++i) {
-      const int at = lane * each + i;
-      if (at < a.n) mine += all_places(sequence_of(a, at));
+    if (each == 1) {
+      if (lane < a.n) {
+        mine_of = sequence_of(a, lane);
+        mine = all_places(mine_of);
+      }
+    } else {                                      // (their lengths asked for at once)
+#pragma unroll
+      for (int i = 0; i < kPlanBatch / 64; ++i) {
+        const int at = lane * each + i, places = all_places(sequence_of(a, min(at, a.n - 1)));
+        mine += i < each && at < a.n ? places : 0;
+      }
     }
     const int upto = (int)wave_scan((uint32_t)mine, sum_of);
-    total = __builtin_amdgcn_readlane(upto, 63);
-    if constexpr (kSplit) run = (total + a.runs - 1) / a.runs;
-    if (group * run >= total) return;
-    const int at = __builtin_ctzll(__ballot(upto > group * run));
-    first = __builtin_amdgcn_readlane(upto - mine, at);
+    of_head = __builtin_amdgcn_readlane(upto, 63);
+    if (kSplit) run = (of_head * a.heads_kv + a.runs - 1) / a.runs;
+    if (group * run >= of_head * a.heads_kv) return;
+    kvh = group * run / of_head;
+    const int pos = group * run - kvh * of_head, at = __builtin_ctzll(__ballot(upto > pos));
+    first = kvh * of_head + __builtin_amdgcn_readlane(upto - mine, at);
     b = at * each;
-    if (kSplit && group == 0 && tid == 0) a.first_place[a.n] = total;
   } else {                                        // the last sequence that begins at or before the run: 64 candidates at a time
-    total = a.first_place[a.n];
-    if constexpr (kSplit) run = (total + a.runs - 1) / a.runs;
-    if (group * run >= total) return;
+    of_head = a.first_place[a.n];
+    if (kSplit) run = (of_head * a.heads_kv + a.runs - 1) / a.runs;
+    if (group * run >= of_head * a.heads_kv) return;
+    kvh = group * run / of_head;
     for (int n = a.n; n > 1;) {
       const int apart = (n + 63) / 64, at = lane * apart;
-      const bool before = at < n && a.first_place[b + min(at, n - 1)] <= group * run;
+      const bool before = at < n && a.first_place[b + min(at, n - 1)] <= group * run - kvh * of_head;
       const int skip = (__builtin_popcountll(__ballot(before)) - 1) * apart;
       b += skip;
       n = min(apart, n - skip);
     }
-    first = a.first_place[b];
+    first = kvh * of_head + a.first_place[b];
   }
-  const int begin = group * run, end = min(begin + run, total);
+  const int begin = group * run, end = min(begin + run, of_head * a.heads_kv);
 
-  for (int pos = begin; pos < end && b < a.n;) {    // (offsets that do not ascend may have places for no one)
-    const Sequence seq = sequence_of(a, b);
+  for (int pos = begin; pos < end;) {
+    if (b >= a.n) {
+      if (++kvh >= a.heads_kv) return;            // (offsets that do not ascend may have places for no one)
+      b = 0;
+    }
+    Sequence seq;
+    if (a.n <= 64) seq = {__builtin_amdgcn_readlane(mine_of.len, b), __builtin_amdgcn_readlane(mine_of.row0, b), __builtin_amdgcn_readlane(mine_of.n, b)};
+    else seq = sequence_of(a, b);
     const int rows = seq.n * a.group, units = tree_units(rows, G::kRowTile), places = places_of(seq);
-    if (pos >= first + units * places * a.heads_kv) {        // (a sequence without rows has no places)
-      first += units * places * a.heads_kv;
+    if (pos >= first + units * places) {          // (a sequence without rows has no places)
+      first += units * places;
       ++b;
       continue;
     }
-    const int index = (pos - first) / places, unit_first = first + index * places;
-    const int kvh = index / units, unit = index - kvh * units, seq_b = b;
-    int t0 = 0, t1 = tree_steps(seq.len, G::kStep), place = 0;
+    const int unit = (pos - first) / places, unit_first = first + unit * places, seq_b = b;
+    const int steps = tree_steps(seq.len, G::kStep);
+    int t0 = 0, t1 = steps, place = 0, last = 0;
     bool whole = true;
     if constexpr (kSplit) {
-      const DecodePiece piece = decode_piece(unit_first, t1, group, run, kLead);
+      const DecodePiece piece = decode_piece(unit_first, steps, group, run, kLead);
       pos = unit_first + places;
       if (piece.t1 <= piece.t0) continue;         // the run ends before its first step
-      whole = piece.t0 == 0 && piece.t1 == t1;
+      whole = piece.t0 == 0 && piece.t1 == steps;
       place = decode_part(piece, group);
       t0 = piece.t0;
       t1 = piece.t1;
-      if (a.n <= kPlanBatch && index == 0 && t0 == 0 && tid == 0) a.first_place[seq_b] = first;
+      if (t0 == 0 && !whole) last = decode_last_group(unit_first, steps, run, kLead);
     } else {
       pos = end;
     }
+    const bool has_first = t0 == 0;               // the unit's first step
     const int base = seq.len - seq.n, unit_rows = min(G::kRowTile, rows - unit * G::kRowTile);
     // no row of a chain sees more than its last one's token
     const int limit = a.masks ? seq.len : max(min(seq.len, base + (int)a.per_token.div(unit * G::kRowTile + unit_rows - 1) + 1), 0);
@@ -524,14 +568,10 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
 
     R rw;
     const uint32_t ring = lds_address(smem), k_lane = R::k_at(lane), v_lane = R::v_at(lane);
-    const int row_first = wave * R::kRows;    // of the unit
+    const int row_first = wave * R::kRows;        // of the unit
     const bool works = row_first < unit_rows;
     const int my_row = unit * G::kRowTile + min(row_first + R::column(lane), unit_rows - 1);
     const int my_token = (int)a.per_token.div(my_row), my_head = kvh * a.group + my_row - my_token * a.group;
-    rw.load_q(a.q + (seq.row0 + my_token) * a.q_t + my_head * a.q_h, lane);
-    __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0), for the compiler to know: it would wait for the queries in the loop, and for the ring with them
-    const uint64_t* const my_mask = a.masks ? a.masks + (seq.row0 + my_token) * a.mask_stride : nullptr;
-
     const int32_t* const table = a.table + (int64_t)seq_b * a.table_stride;
     const char* const k_head = a.k + kvh * a.k_h;
     const char* const v_head = a.v + kvh * a.v_h;
@@ -541,6 +581,17 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
       for (int i = wave; i < kWindow / 64; i += kWaves)
         word_to_lds(table + min(p0 + 64 * i + lane, last), ring + G::kIdsAt + ((window & 1) * kWindow + 64 * i) * 4);
     };
+    const int window0 = t0 * G::kStep / kWindow;
+    if (t0 < t1) {
+      fetch_ids(window0);
+      fetch_ids(window0 + 1);
+    }
+    rw.load_q(a.q + (seq.row0 + my_token) * a.q_t + my_head * a.q_h, lane);
+    // the first two words of the row's mask, all of them as a rule
+    const uint64_t* const my_mask = a.masks ? a.masks + (seq.row0 + my_token) * a.mask_stride : nullptr;
+    const uint64_t mask0 = a.masks ? my_mask[0] : 0, mask1 = a.masks && a.words > 1 ? my_mask[1] : 0;
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0), for the compiler to know: it would wait for the queries in the loop, and for the ring with them
     auto place_tokens = [&](int window) {         // everyone is there before and after
       const int side = window & 1, tok0 = window * kWindow, p0 = (int)a.page.div(tok0);
 #pragma unroll
@@ -572,13 +623,17 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
       }
     };
     // Every step in turn: body(step, place of its K in the LDS, next), which has everyone call next() once.
+    bool again = false;
     auto traverse = [&](auto body) {
-      int placed = t0 * G::kStep / kWindow;       // the last window whose tokens' places are there
+      int placed = window0;                       // the last window whose tokens' places are there
       int stage_to = 0, stage_at = 0;
       if (t0 < t1) {
-        fetch_ids(placed);
-        fetch_ids(placed + 1);
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (again) {
+          fetch_ids(placed);
+          fetch_ids(placed + 1);
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        again = true;
         meet();
         place_tokens(placed);
         meet();
@@ -616,7 +671,8 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
         s.bits = chain_bits(my_token, at);
         if (my_mask) {
           const int w = max(at, 0) >> 6;
-          s.bits = tree_bits(w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
+          if (w == 0) s.bits = tree_bits(mask0, mask1, at);
+          else s.bits = tree_bits(w == 1 ? mask1 : w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
         }
         s.bits &= live;
       }
@@ -667,16 +723,16 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves>::kWavesPe
 
     const float sum = rw.whole_sum();
     const int row = row_first + R::column(lane);  // of the unit
-    if (row < unit_rows) {
-      if (whole) {
-        char* const to = a.out + (seq.row0 + my_token) * a.out_t + my_head * a.out_h;
-        rw.each(lane, [&](int dim, floatx4 o) { store4<kBf16>(to + dim * kElem, normalised(o, sum)); });
-        if (a.lse && R::writes_sum(lane)) a.lse[(int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head] = lse_of(rw.m, sum);
-      } else {
-        const int64_t to = (int64_t)place * G::kRowTile + row;
-        rw.each(lane, [&](int dim, floatx4 o) { *reinterpret_cast<floatx4*>(a.part_o + to * kD + dim) = o; });
-        if (R::writes_sum(lane)) a.part_ml[to] = make_float2(rw.m, sum);
-      }
+    const bool there = row < unit_rows;
+    const int64_t id = (int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head;
+    if (kSplit && has_first && there && R::writes_sum(lane)) a.cut_of[id] = whole ? -1 : pack_cut(group, last, row);
+    if (whole) {
+      rw.store(a.out + (seq.row0 + my_token) * a.out_t + my_head * a.out_h, sum, lane, there);
+      if (a.lse && there && R::writes_sum(lane)) a.lse[id] = lse_of(rw.m, sum);
+    } else if (there) {
+      const int64_t to = (int64_t)place * G::kRowTile + row;
+      rw.each(lane, [&](int dim, floatx4 o) { *reinterpret_cast<floatx4*>(a.part_o + to * kD + dim) = o; });
+      if (R::writes_sum(lane)) a.part_ml[to] = make_float2(rw.m, sum);
     }
     if constexpr (kSplit) meet();
   }
@@ -688,7 +744,7 @@ __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs a, int step, i
   const int tid = threadIdx.x, each = (a.n + 1023) / 1024, i0 = min(tid * each, a.n), i1 = min(i0 + each, a.n);
   auto places = [&](int i) {
     const Sequence s = sequence_of(a, i);
-    return tree_units(s.n * a.group, tile) * (split ? tree_steps(s.len, step) + tree_lead(step) : 1) * a.heads_kv;
+    return tree_units(s.n * a.group, tile) * (split ? tree_steps(s.len, step) + tree_lead(step) : 1);
   };
   int mine = 0;
   for (int i = i0; i < i1; ++i) mine += places(i);
@@ -705,51 +761,56 @@ __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs a, int step, i
   if (tid == 1023) a.first_place[a.n] = at;
 }
 
-// The pieces of a row that more than one workgroup had a part in, added up: 4 numbers to a lane, a part to every d / 4 lanes.
+// The pieces of a row that more than one workgroup had a part in, added up, a wave to a row: 4 numbers to a lane, a part to every d / 4 lanes, four of them asked for at once.  In the
+// order of heads that the runs have, so that a row is added up where its parts were made, whose L2 has them: one sequence of 700 tokens, 22 parts to a row, 9.7 us in the order of
+// rows, 5.6 in this.
+constexpr int kJoinThreads = 256;
 template <bool kBf16, int kD>
-__global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int step, int tile) {
-  constexpr int kLanes = kD / 4, kParts = 64 / kLanes, kElem = kBf16 ? 2 : 4;
-  const int lane = threadIdx.x & 63, heads_q = a.heads_kv * a.group;
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= (int64_t)a.tokens * heads_q) return;
-  const int t = (int)(id / heads_q), head = (int)(id - (int64_t)t * heads_q);
-  if (t < a.cu[0] || t >= a.cu[a.n]) return;
-  int b = 0;                                  // the last sequence that begins at or before the row
-  for (int n = a.n; n > 1;) {
-    const int apart = (n + 63) / 64, at = lane * apart;
-    const bool before = at < n && a.cu[b + min(at, n - 1)] <= t;
-    const int skip = max((int)__builtin_popcountll(__ballot(before)) - 1, 0) * apart;
-    b += skip;
-    n = min(apart, n - skip);
-  }
-  const Sequence s = sequence_of(a, b);
-  if (t < s.row0 || t >= s.row0 + s.n) return;
-  const int lead = tree_lead(step), steps = tree_steps(s.len, step), total = a.first_place[a.n], run = (total + a.runs - 1) / a.runs;
-  const int kvh = head / a.group, r = (t - s.row0) * a.group + head - kvh * a.group, unit = r / tile, row = r - unit * tile;
-  const int first = a.first_place[b] + (kvh * tree_units(s.n * a.group, tile) + unit) * (steps + lead);
-  const int g0 = decode_first_group(first, run, lead), g1 = decode_last_group(first, steps, run, lead);
-  if (g0 == g1 || g0 < 0 || g1 >= a.runs) return;      // (whole; or offsets that do not ascend)
-  const int c = lane % kLanes;
+__global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeArgs a, int tile, int groups) {
+  constexpr int kLanes = kD / 4, kSubs = 64 / kLanes, kRows = kJoinThreads / 64, kElem = kBf16 ? 2 : 4, kParts = 4;
+  const int lane = threadIdx.x & 63, c = lane % kLanes, rows = a.tokens * a.group, of_head = (rows + kRows - 1) / kRows;
+  const int group = (blockIdx.x & 7) * (groups >> 3) + (blockIdx.x >> 3), kvh = group / of_head, r = (group - kvh * of_head) * kRows + (threadIdx.x >> 6);
+  if (kvh >= a.heads_kv || r >= rows) return;
+  const int t = (int)a.per_token.div(r), head = kvh * a.group + r - t * a.group;
+  const int64_t id = (int64_t)t * a.heads_kv * a.group + head;
+  const int cut = a.cut_of[id], begin = a.cu[0], end = a.cu[a.n];
+  const int g0 = cut & (kMostRuns - 1), g1 = min(cut / kMostRuns & (kMostRuns - 1), a.runs - 1), row = cut / (kMostRuns * kMostRuns);
+  if (cut < 0 || t < begin || t >= end || row >= tile) return;       // (a row of no sequence has anything there)
   float m = -INFINITY, l = 0.f;
   floatx4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int w = g0 + lane / kLanes; w <= g1; w += kParts) {
-    const int64_t place = (int64_t)decode_part(decode_piece(first, steps, w, run, lead), w) * tile + row;
-    const float2 ml = a.part_ml[place];
-    const floatx4 p = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
-    const float top = fmaxf(m, ml.x), f = factor_of(m, top), x = factor_of(ml.x, top);
+  for (int w0 = g0 + lane / kLanes; w0 <= g1; w0 += kSubs * kParts) {
+    float2 ml[kParts];
+    floatx4 p[kParts];
+#pragma unroll
+    for (int j = 0; j < kParts; ++j) {
+      // place 1 of the run that it begins in, place 0 of the others
+      const int w = min(w0 + j * kSubs, g1);
+      const int64_t place = (int64_t)(2 * w + (w == g0)) * tile + row;
+      ml[j] = a.part_ml[place];
+      p[j] = *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c);
+    }
+    float top = m;
+#pragma unroll
+    for (int j = 0; j < kParts; ++j) top = fmaxf(top, ml[j].x);
+    const float old = factor_of(m, top);
     m = top;
-    l = l * f + ml.y * x;
-    o = o * f + p * x;
+    l *= old;
+    o *= old;
+#pragma unroll
+    for (int j = 0; j < kParts; ++j) {
+      if (w0 + j * kSubs > g1) break;
+      const float f = factor_of(ml[j].x, top);
+      l = fmaf(ml[j].y, f, l);
+      o += p[j] * f;
+    }
   }
 #pragma unroll
   for (int off = kLanes; off < 64; off *= 2) {
     const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), top = fmaxf(m, m2), f = factor_of(m, top), x = factor_of(m2, top);
-    floatx4 o2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o2[i] = __shfl_xor(o[i], off);
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * f + __shfl_xor(o[i], off) * x;
     m = top;
     l = l * f + l2 * x;
-    o = o * f + o2 * x;
   }
   if (lane >= kLanes) return;
   store4<kBf16>(a.out + t * a.out_t + head * a.out_h + c * 4 * kElem, normalised(o, l));
@@ -760,7 +821,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, int step, in
 struct Variant { int waves, tile, step, runs; };
 template <bool kBf16, int kD, int kWaves>
 constexpr Variant variant() {
-  using G = Geometry<kBf16, kD, kWaves>;
+  using G = Geometry<kBf16, kD, kWaves, true>;
   return {kWaves, G::kRowTile, G::kStep, 256 * G::kGroups};
 }
 // f(bf16, d, waves) of a call as constants
@@ -772,9 +833,17 @@ auto with_waves(bool bf16, int d, int waves, F f) {
   };
   return waves == 2 ? pick(std::integral_constant<int, 2>{}) : waves == 4 ? pick(std::integral_constant<int, 4>{}) : pick(std::integral_constant<int, 8>{});
 }
-Variant variant_of(int tokens, int n, int group, int d, bool bf16) {
+// Short sequences are not cut: a workgroup for a unit, and no join.  Of 64 / 8 sequences (8 KV heads, 8 new tokens), not cut and cut: bf16, d = 128, 500 tokens 43 / 20 us
+// and 33 / 16, 120 tokens 14 / 10.5 and 18 / 10.5; d = 64, 490 tokens 20.8 / 17.1 and 28.1 / 13.6; f32, d = 64, 230 tokens 32 / 18.5 and 37 / 15, d = 128, 110 tokens 45 / 19 and 30 / 15.
+bool is_solo(int row_tokens, int d, bool bf16) { return (int64_t)row_tokens * d <= (bf16 ? 32768 : 8192); }
+// Two waves where they have all of the rows, and where more workgroups to a compute unit can be had for it: f32, d = 128, 16 sequences of 4000, 32 rows 142 us, and 166 of four
+// waves; but bf16 at d = 128 124 us of 4 rows, and 117 of four waves, whose ring is as large and is filled by more.  Eight, once four have too few rows: of 128 rows (bf16, d = 128,
+// 32 sequences of 1000 to 16000) 193 us with four waves, 227 with eight; of 192 290 with either.
+constexpr int least_waves(bool bf16, int d, bool split) { return bf16 && d == 128 && split ? 4 : 2; }
+Variant variant_of(int tokens, int n, int group, int d, bool bf16, int row_tokens) {
   const int64_t wave_rows = bf16 ? 32 : 16, rows = ((int64_t)tokens * group + n - 1) / n;
-  return with_waves(bf16, d, rows <= wave_rows ? 2 : rows <= 3 * wave_rows ? 4 : 8, [](auto b, auto d, auto w) {
+  const int least = least_waves(bf16, d, !is_solo(row_tokens, d, bf16));
+  return with_waves(bf16, d, rows <= 2 * wave_rows ? least : rows <= 4 * wave_rows ? 4 : 8, [](auto b, auto d, auto w) {
     return variant<decltype(b)::value, decltype(d)::value, decltype(w)::value>();
   });
 }
@@ -784,12 +853,12 @@ int64_t most_units(int tokens, int n, int heads_kv, int group, int tile) {
 int64_t most_places(int tokens, int n, int heads_kv, int group, const Variant& v, int row_tokens) {
   return most_units(tokens, n, heads_kv, group, v.tile) * (tree_steps(row_tokens, v.step) + tree_lead(v.step));
 }
-bool is_solo(int64_t units, int row_tokens) { return row_tokens <= 512; }
-struct TreeWs { size_t first_place, part_o, part_ml, total; };
-TreeWs carve(int n, int64_t runs, int tile, int d) {
+struct TreeWs { size_t first_place, cut_of, part_o, part_ml, total; };
+TreeWs carve(int n, int64_t rows, int64_t runs, int tile, int d) {
   TreeWs w;
   size_t o = 0;
   w.first_place = o; o += align_up((size_t)(n + 1) * 4, 256);
+  w.cut_of = o; o += align_up((size_t)(runs ? rows : 0) * 4, 256);
   w.part_o = o; o += align_up((size_t)2 * runs * tile * d * 4, 256);
   w.part_ml = o; o += align_up((size_t)2 * runs * tile * 8, 256);
   w.total = o;
@@ -798,7 +867,7 @@ TreeWs carve(int n, int64_t runs, int tile, int d) {
 
 template <bool kBf16, int kD, int kWaves, bool kSplit>
 basa_status launch_kernel(const TreeArgs& a, hipStream_t st) {
-  using G = Geometry<kBf16, kD, kWaves>;
+  using G = Geometry<kBf16, kD, kWaves, kSplit>;
   const auto kernel = tree_kernel<kBf16, kD, kWaves, kSplit, true>;
   if (a.n > kPlanBatch) {
     ProfScope prof(K_TREE, st);
@@ -814,13 +883,16 @@ basa_status launch_kernel(const TreeArgs& a, hipStream_t st) {
 }
 template <bool kBf16, int kD, int kWaves>
 basa_status launch(const TreeArgs& a, bool solo, hipStream_t st) {
-  using G = Geometry<kBf16, kD, kWaves>;
+  using G = Geometry<kBf16, kD, kWaves, true>;
   if (solo) return launch_kernel<kBf16, kD, kWaves, false>(a, st);
-  const basa_status s = launch_kernel<kBf16, kD, kWaves, true>(a, st);
+  basa_status s = BASA_OK;
+  if constexpr (kWaves >= least_waves(kBf16, kD, true)) s = launch_kernel<kBf16, kD, kWaves, true>(a, st);
   if (s != BASA_OK) return s;
   ProfScope prof(K_TREE_JOIN, st);
-  const int64_t rows = (int64_t)a.tokens * a.heads_kv * a.group;
-  tree_join_kernel<kBf16, kD><<<(int)((rows + 3) / 4), 256, 0, st>>>(a, G::kStep, G::kRowTile);
+  static_assert(256 * G::kGroups <= kMostRuns && G::kRowTile <= kMostRows, "a packed cut");
+  constexpr int kRows = kJoinThreads / 64;
+  const int groups = (int)align_up((size_t)a.heads_kv * ceil_div(a.tokens * a.group, kRows), 8);
+  tree_join_kernel<kBf16, kD><<<groups, kJoinThreads, 0, st>>>(a, G::kRowTile, groups);
   BASA_HIP_CHECK_LAUNCH("tree_join_kernel");
   return BASA_OK;
 }
@@ -829,14 +901,14 @@ basa_status launch(const TreeArgs& a, bool solo, hipStream_t st) {
 
 bool tree_takes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens) {
   const int group = heads_q / heads_kv;
-  return n == 0 || most_places(tokens, n, heads_kv, group, variant_of(tokens, n, group, d, bf16), row_tokens) < INT_MAX / 2;
+  return n == 0 || most_places(tokens, n, heads_kv, group, variant_of(tokens, n, group, d, bf16, row_tokens), row_tokens) < INT_MAX / 2;
 }
 size_t tree_workspace_bytes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens) {
   if (n == 0) return 256;
   const int group = heads_q / heads_kv;
-  const Variant v = variant_of(tokens, n, group, d, bf16);
-  if (is_solo(most_units(tokens, n, heads_kv, group, v.tile), row_tokens)) return carve(n, 0, 0, 0).total;
-  return carve(n, std::min<int64_t>(v.runs, most_places(tokens, n, heads_kv, group, v, row_tokens)), v.tile, d).total;
+  const Variant v = variant_of(tokens, n, group, d, bf16, row_tokens);
+  if (is_solo(row_tokens, d, bf16)) return carve(n, 0, 0, 0, 0).total;
+  return carve(n, (int64_t)tokens * heads_q, std::min<int64_t>(v.runs, most_places(tokens, n, heads_kv, group, v, row_tokens)), v.tile, d).total;
 }
 
 // Tokens' places are 32-bit numbers, in units of the largest power of two up to 256 that divides the strides of pages and tokens, in bytes: 16 at least, and
@@ -874,14 +946,15 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
   a.per_token = fast_div((uint32_t)a.group);
   a.masks = reinterpret_cast<const uint64_t*>(masks); a.words = words; a.mask_stride = mask_stride;
   a.out = static_cast<char*>(out); a.out_t = out_st * e; a.out_h = out_sh * e; a.lse = lse;
-  const Variant v = variant_of(a.tokens, n, a.group, q.d, bf16);
+  const Variant v = variant_of(a.tokens, n, a.group, q.d, bf16, a.row_tokens);
   const int64_t units = most_units(a.tokens, n, a.heads_kv, a.group, v.tile);
-  const bool solo = is_solo(units, a.row_tokens);
+  const bool solo = is_solo(a.row_tokens, q.d, bf16);
   a.runs = solo ? 0 : (int)std::min<int64_t>(v.runs, most_places(a.tokens, n, a.heads_kv, a.group, v, a.row_tokens));
   a.groups = (int)align_up(solo ? units : a.runs, 8);
-  const TreeWs w = carve(n, a.runs, v.tile, q.d);
+  const TreeWs w = carve(n, (int64_t)q.L * q.heads, a.runs, v.tile, q.d);
   char* base = static_cast<char*>(ws);
   a.first_place = reinterpret_cast<int*>(base + w.first_place);
+  a.cut_of = reinterpret_cast<int*>(base + w.cut_of);
   a.part_o = reinterpret_cast<float*>(base + w.part_o);
   a.part_ml = reinterpret_cast<float2*>(base + w.part_ml);
   a.scale_log2e = 1.4426950408889634f / sqrtf((float)q.d);

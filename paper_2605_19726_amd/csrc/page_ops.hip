@@ -414,7 +414,7 @@ __global__ __launch_bounds__(1024) void free_list_kernel(FreeArgs a, int words_e
   const int first = blockIdx.x * words_each, n = min(words_each, a.words - first), tid = threadIdx.x;
   int mine = 0;
   const uintx4* const bytes = reinterpret_cast<const uintx4*>(a.used);
-  constexpr int kLoads = 4;
+  constexpr int kLoads = 8;
   for (int c0 = 0; c0 < 2 * first; c0 += 1024 * kLoads) {     // 16 pages each
     uintx4 x[kLoads];
 #pragma unroll

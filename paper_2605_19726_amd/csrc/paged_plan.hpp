@@ -68,7 +68,7 @@ inline int decode_groups(int64_t most) { return (int)(most < kDecodeMost ? most 
 
 // ---- several new tokens of every sequence -----------------------------------------------------------
 // The same axis for attention whose rows are (new token, query head) pairs: a (sequence, KV head) has a unit for every `tile` of its rows, none if
-// there are none; the units lie in the order sequence, head, tile, each with places as above, for steps of `step` tokens.
+// there are none; the units lie in the order head, sequence, tile, each with places as above, for steps of `step` tokens.
 BASA_HD constexpr int tree_lead(int step) { return step < kDecodeStep ? kDecodeStep / step : 1; }
 BASA_HD int tree_steps(int len, int step) { return len <= step ? 1 : (len + step - 1) / step; }
 BASA_HD int tree_units(int rows, int tile) { return (rows + tile - 1) / tile; }
