@@ -133,6 +133,20 @@ def test_long_sequences_are_split_and_joined(dtype, hq, hk, lens, new, chain):
     c.check(*c.run(), f"{dtype} {hq}/{hk} {lens}")
 
 
+# rows of the table with room for 64 to 512 tokens: up to some number of them sequences are not cut, and few rows have rings of two steps
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("room", [64, 80, 128, 144, 256, 272, 512, 528])
+@pytest.mark.parametrize("n,new", [(1, 5), (3, 17), (70, 2)])
+def test_short_sequences(dtype, d, room, n, new):
+    rng = np.random.default_rng(room + n)
+    lens = rng.integers(new, room + 1, n)
+    lens[0] = room
+    count = rng.integers(0, new + 1, n)
+    count[0] = new
+    c = Case(dtype, d, 10, 5, 16, lens.tolist(), count.tolist(), room + new, width=room // 16)
+    c.check(*c.run(), f"{dtype} d={d} room for {room}, {n} sequences, {new} new")
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("n,width", [(513, 8), (700, 40)])
 def test_many_sequences_in_a_mixed_step(dtype, n, width):
