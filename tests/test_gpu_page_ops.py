@@ -198,6 +198,21 @@ def test_free_of_large_pools(n, width, page, pages):
     _free_check(table, rng.integers(0, page * width + 1, n), page, pages)
 
 
+# rows from one entry to more than a wave has lanes, on both sides of one workgroup
+@pytest.mark.parametrize("n,width", [(1, 1), (17, 1), (1000, 2), (5000, 1), (1500, 3), (1025, 32), (500, 33), (512, 63), (513, 64), (255, 65), (257, 65), (300, 129), (2, 9000)])
+def test_free_of_narrow_and_wide_rows(n, width):
+    rng = np.random.default_rng(n + width)
+    pages = n * width + 77
+    table = rng.integers(-2, pages + 2, (n, width)).astype(np.int32)                  # none, others' pages, pages twice
+    _free_check(table, rng.integers(-1, 16 * width + 20, n), 16, pages)
+    wide = np.full((n, width + 3), 5, dtype=np.int32)
+    wide[:, :width] = table
+    lens = rng.integers(0, 16 * width + 1, n)
+    free, count = bd.basa_page_free(ints(wide)[:, :width], ints(lens), 16, pages)
+    want = free_pages(table, lens, 16, pages)
+    assert int(count) == len(want) and np.array_equal(free[:len(want)].cpu().numpy(), np.array(want, dtype=np.int32))
+
+
 def test_free_without_sequences():
     for pages in (50, 2 ** 19):
         free, count = bd.basa_page_free(ints(np.zeros((0, 4))), ints([]), 16, pages)
