@@ -837,13 +837,14 @@ auto with_waves(bool bf16, int d, int waves, F f) {
 // and 33 / 16, 120 tokens 14 / 10.5 and 18 / 10.5; d = 64, 490 tokens 20.8 / 17.1 and 28.1 / 13.6; f32, d = 64, 230 tokens 32 / 18.5 and 37 / 15, d = 128, 110 tokens 45 / 19 and 30 / 15.
 bool is_solo(int row_tokens, int d, bool bf16) { return (int64_t)row_tokens * d <= (bf16 ? 32768 : 8192); }
 // Two waves where they have all of the rows, and where more workgroups to a compute unit can be had for it: f32, d = 128, 16 sequences of 4000, 32 rows 142 us, and 166 of four
-// waves; but bf16 at d = 128 124 us of 4 rows, and 117 of four waves, whose ring is as large and is filled by more.  Eight, once four have too few rows: of 128 rows (bf16, d = 128,
-// 32 sequences of 1000 to 16000) 193 us with four waves, 227 with eight; of 192 290 with either.
+// waves; but bf16 at d = 128 124 us of 4 rows, and 117 of four waves, whose ring is as large and is filled by more.  Four or eight: the fewer rows that
+// the last tile leaves empty.  Of 128 rows (bf16, d = 128, 32 sequences of 1000 to 16000) 193 us with four waves, 227 with eight; of 192 290 with either; of 288 469 and 482, but of
+// 640 850 and 819, 1152 1506 and 1405: bf16 takes four for up to three tiles only.  f32 (16 sequences of 2000): 144 rows 252 and 320, 320 436 and 483, 832 1152 and 1190.
 constexpr int least_waves(bool bf16, int d, bool split) { return bf16 && d == 128 && split ? 4 : 2; }
 Variant variant_of(int tokens, int n, int group, int d, bool bf16, int row_tokens) {
   const int64_t wave_rows = bf16 ? 32 : 16, rows = ((int64_t)tokens * group + n - 1) / n;
   const int least = least_waves(bf16, d, !is_solo(row_tokens, d, bf16));
-  return with_waves(bf16, d, rows <= 2 * wave_rows ? least : rows <= 4 * wave_rows ? 4 : 8, [](auto b, auto d, auto w) {
+  return with_waves(bf16, d, rows <= 2 * wave_rows ? least : (!bf16 || rows <= 12 * wave_rows) && align_up(rows, 8 * wave_rows) > align_up(rows, 4 * wave_rows) ? 4 : 8, [](auto b, auto d, auto w) {
     return variant<decltype(b)::value, decltype(d)::value, decltype(w)::value>();
   });
 }
