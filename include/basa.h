@@ -362,7 +362,7 @@ basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, c
  * A step (basa_page_tables) in which sequence i gets n_i tokens, rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 of the packed batch.  They may be a tree: token r follows
  * token parents[r] of its sequence's new ones, or the context.  They enter the pages in their order (basa_cache_append), attend to the context and their
  * own ancestors (basa_tree_attn), and once some are accepted, the kept ones are moved together (basa_cache_compact) and the sequence is
- * as long as that.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending.
+ * as long as that.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending.  n_seq is up to 2^22.
  */
 
 /*
@@ -405,7 +405,7 @@ basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, con
  *   start, count [n_seq] int32; counts beyond `most` count as that.
  *   keep         [n_seq, most] int32, rows keep_stride >= most entries apart; the first count[i] of a row ascend strictly from 0 or more on.  (Of other lists it is
  *                not defined which rows are moved; an entry below its own place, a place without a page or beyond the table row moves nothing.)
- * The pages that are written to must belong to their sequence alone.  What stood behind the kept tokens stays there.
+ * The pages that are written to must belong to their sequence alone.  What stood behind the kept tokens stays there.  n_seq * heads * bytes of a row < 2^29.
  */
 basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
                                const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,

@@ -428,6 +428,7 @@ basa_status check_tree(const basa_tensor* q, const basa_tensor* k, const basa_te
     set_error("query heads (%d) must be a multiple of kv heads (%d)", q->heads, k->heads); return BASA_ERR_INVALID_ARG;
   }
   if (n_seq < 0) { set_error("negative number of sequences (%d)", n_seq); return BASA_ERR_INVALID_ARG; }
+  if (n_seq > kMaxDecodeRows) { set_error("more than %d sequences in a call", kMaxDecodeRows); return BASA_ERR_UNSUPPORTED; }
   if ((int64_t)q->L * q->heads > kMaxTreeRows) { set_error("q: tokens*heads exceeds %d", kMaxTreeRows); return BASA_ERR_UNSUPPORTED; }
   if (tree_place_unit(view_of(*k), view_of(*v)) < 0) { set_error("pages that reach further than the tokens' places do (2^32 times a row)"); return BASA_ERR_UNSUPPORTED; }
   if ((s = check_width(width, k->L)) != BASA_OK) return s;
@@ -865,6 +866,7 @@ basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, i
                             int64_t mask_stride, int32_t* depths, void* stream) {
   if (n_seq < 0 || tokens < 0) { set_error("negative number of sequences (%d) or tokens (%d)", n_seq, tokens); return BASA_ERR_INVALID_ARG; }
   if (tokens > kMaxPagedTokens) { set_error("more than %d tokens in a call", kMaxPagedTokens); return BASA_ERR_UNSUPPORTED; }
+  if (n_seq > kMaxDecodeRows) { set_error("more than %d sequences in a call", kMaxDecodeRows); return BASA_ERR_UNSUPPORTED; }
   if (words < 1) { set_error("masks need words >= 1 (got %d)", words); return BASA_ERR_INVALID_ARG; }
   if (words > kMaxMaskWords) { set_error("more than %d words to a mask (%d)", kMaxMaskWords, words); return BASA_ERR_UNSUPPORTED; }
   if (mask_stride < words) { set_error("rows of masks are %lld words apart, %d wide", (long long)mask_stride, words); return BASA_ERR_INVALID_ARG; }
@@ -923,6 +925,9 @@ basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_
   if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
   if (most < 0 || keep_stride < most) { set_error("rows of keep are %lld entries apart, %d wide", (long long)keep_stride, most); return BASA_ERR_INVALID_ARG; }
   if (n_seq > 0 && most > 0 && (!start || !keep || !count)) { set_error("null start, keep or count"); return BASA_ERR_INVALID_ARG; }
+  if (!compact_takes(n_seq, view_of(*k_pages), most)) {
+    set_error("%d sequences of %d heads: more than a call takes", n_seq, k_pages->heads); return BASA_ERR_UNSUPPORTED;
+  }
   return launch_cache_compact(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, start, keep, most, keep_stride, count, n_seq,
                               reinterpret_cast<hipStream_t>(stream));
 }

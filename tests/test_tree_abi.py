@@ -112,6 +112,17 @@ def test_page_free(lib):  # noqa: F811
     assert lib.basa_page_free_workspace_size(10, 20, 0) == 0 and lib.basa_page_free_workspace_size(0, 20, 2 ** 20) >= 2 ** 17
 
 
+def test_more_sequences_than_a_launch_has_groups_for_are_refused(lib):  # noqa: F811
+    many = 2 ** 22 + 1
+    assert status_of(lib, lib.basa_tree_masks, V(2 ** 40), V(2 ** 41), many, 100, V(2 ** 42), 1, 1, None, None)[0] == UNSUPPORTED
+    far = dict(table=2 ** 50, lens=2 ** 51, cu=2 ** 52, masks=None)
+    assert _tree(lib, n=many, **far) == UNSUPPORTED
+    compact = lambda k, n, most: status_of(lib, lib.basa_cache_compact, C.byref(k), C.byref(k), V(2 ** 40), 10, 10, V(2 ** 41), V(2 ** 42), most, most, V(2 ** 43), n, None)[0]  # noqa: E731
+    assert compact(pages(), many, 6) == UNSUPPORTED and compact(pages(), many, 600) == UNSUPPORTED
+    wide = pages(heads=2 ** 15, stride_l=2 ** 22, stride_h=128, stride_b=2 ** 26)
+    assert compact(wide, 2 ** 16, 600) == UNSUPPORTED                  # 2^16 sequences of 2^16 lines of K and of V
+
+
 def test_the_binding_refuses_what_the_kernels_would_misread():
     z = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype)  # noqa: E731
     cache = bd.PagedCache(*(torch.zeros(6, 2, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
