@@ -18,7 +18,7 @@ __device__ __forceinline__ int pages_of(const FastDiv& page, int tokens) {
 // ---- who sees whom ---------------------------------------------------------------------------------
 // M(r) = {r} u M(p(r)): in two steps.  Within a run of 64 tokens, one wave: bits and the way out (the first ancestor before the run) by doubling, six
 // rounds of lane exchanges.  Then a token's row is its own run's bits, those of its way out, and so on: at most one step per 64 tokens.
-// Bound by latency.
+// Bound by latency: 2.6 us of 8 sequences of 25 tokens, as long as the shortest kernel takes; 3.9 of 200 ragged ones.
 __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* parents, const int32_t* cu, int tokens, uint64_t* masks, int words,
                                                          int64_t mask_stride, int32_t* depths) {
   extern __shared__ __attribute__((aligned(16))) uint64_t run_bits[];      // [64 words], then the ways out
@@ -88,7 +88,7 @@ __device__ __forceinline__ Move move_of(const CompactArgs& a, int seq, int start
   return {from_id * page_bytes + (from - (int64_t)from_page * a.page.d) * row_bytes, to_id * page_bytes + (to - (int64_t)to_page * a.page.d) * row_bytes};
 }
 
-// Short lists, the paths of trees: a lane to every 16 bytes of a token.  Bound by latency.
+// Short lists, the paths of trees: a lane to every 16 bytes of a token.  Bound by latency: 3.5 us of 64 sequences with paths of some 5 of 16 tokens.
 constexpr int kMoves = 256, kAtOnce = 8;
 __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
   __shared__ Move moves[2][kMoves];         // K, V
@@ -122,7 +122,7 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
 
 // Long lists: a workgroup to every 128 bytes of a token's K or V, eight lanes to a row, eight rows to each of them read before one is written, a move to every thread.  The
 // next rows are read while these are written; what their places come from was asked for a turn and two turns earlier.  Bound by the memory, or by the longest list, whose
-// workgroups take turn after turn.
+// workgroups take turn after turn: 12 sequences of 2000 to 16000 tokens, two thirds kept, 446 MB in 120 us, 3.7 TB/s (a lane to 16 bytes, as for short lists: 2400 us).
 constexpr int kLine = 128, kLinesAtOnce = 8;
 template <int kThreads>
 __global__ __launch_bounds__(kThreads, 4) void compact_lines_kernel(CompactArgs a) {
@@ -203,13 +203,14 @@ __global__ __launch_bounds__(kThreads, 4) void compact_lines_kernel(CompactArgs 
   for (int j0 = kThreads; turn(x, y, j0) && turn(y, x, j0 + kThreads); j0 += 2 * kThreads) {
   }
 }
-// Up to this many moves a list is short.
-constexpr int kShortList = 64;
+// Which lists are short: a workgroup to a line costs 5 ns whatever it moves, a lane that goes down a list waits 0.1 us for eight moves while there is no other to run.  Short / long, of 8
+// sequences (8 heads, d = 128, bf16) lists of 64 10.6 / 8.1 us; of 64 sequences 43 8.9 / 13.3, 85 15.6 / 14.9, 171 30 / 20; of 200 85 24 / 43, 171 55.3 / 55.4, 343 124 / 98.
+bool is_short(int most, int64_t lines) { return most <= 48 + lines / 48; }
 
 // ---- sequences that go on from others --------------------------------------------------------------
 // New sequence j shares the whole pages of its parent.  The page that is not full, if there is one, goes to the first new sequence of the parent; each
 // further one gets the next of the free pages, and a copy of its tokens to make.  Every workgroup finds the first ones (a minimum, whatever the order of
-// its parts) and the running sum of the pages for itself, then writes its rows.
+// its parts) and the running sum of the pages for itself, then writes its rows.  Bound by latency: 3.7 us of 64 from 8, 5.8 of 512 from 512.
 struct ForkArgs {
   const int32_t *table, *lens, *parents, *free_pages;
   int64_t table_stride, new_stride;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256) void page_fork_kernel(ForkArgs a) {
   }
 }
 
-// The first tokens of a page to the same places of another: a 16-byte chunk of K and of V to a lane, in the order of memory.
+// The first tokens of a page to the same places of another: a 16-byte chunk of K and of V to a lane, in the order of memory.  56 copies of up to 64 tokens 4.5 us.
 struct CopyArgs {
   char *k, *v;
   int64_t k_b, k_h, k_l, v_b, v_h, v_l;     // bytes
@@ -307,7 +308,8 @@ __global__ __launch_bounds__(256) void cache_copy_kernel(CopyArgs a) {
 }
 
 // ---- the pages that no one holds -------------------------------------------------------------------
-// A bit for every page, set by the table rows as far as their lengths need pages; then the ids whose bit is not set, in order.
+// A bit for every page, set by the table rows as far as their lengths need pages; then the ids whose bit is not set, in order.  Bound by latency: 6.7 us in one workgroup of
+// 64 sequences of up to 500 pages, three launches of 2.2, 5.0 and 7.7 us of 2000 of up to 1250.
 struct FreeArgs {
   const int32_t *table, *lens;
   int64_t table_stride;
@@ -484,7 +486,8 @@ basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, 
 // A launch has less than 2^32 threads.
 bool compact_takes(int n, const TensorView& k, int most) {
   const int64_t row_lines = k.d * (k.dtype == BASA_BF16 ? 2 : 4) / kLine;
-  return n <= 1 << 22 && (most <= kShortList || n * row_lines * k.heads * 2 < (1 << 23));
+  const int64_t lines = n * row_lines * k.heads * 2;
+  return n <= 1 << 22 && (is_short(most, lines) || lines < (1 << 23));
 }
 basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
                                  const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
@@ -500,15 +503,16 @@ basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_
   while ((1 << a.row_bits) < k_pages.d * e) ++a.row_bits;
   a.page = fast_div((uint32_t)k_pages.L);
   ProfScope prof(K_PAGED, st);
-  if (most <= kShortList) {
+  const int64_t lines = ((int64_t)n * k_pages.heads * 2) << (a.row_bits - 7);
+  if (is_short(most, lines)) {
     a.parts = k_pages.heads << (a.row_bits - 4);
     compact_kernel<<<dim3(n, ceil_div(2 * a.parts, 256)), 256, 0, st>>>(a);
     BASA_HIP_CHECK_LAUNCH("compact_kernel");
   } else {
     a.parts = k_pages.heads << (a.row_bits - 7);
-    const unsigned groups = (unsigned)n * 2 * a.parts;
-    if (groups >= 512) compact_lines_kernel<512><<<groups, 512, 0, st>>>(a);
-    else compact_lines_kernel<1024><<<groups, 1024, 0, st>>>(a);
+    // few long lists: large turns, fewer of them (one of 40000 tokens 118 -> 112 us, 15 of 1000 to 8000 51.6 -> 49.4; but 64 of 1500 90 -> 94)
+    if (lines >= 512) compact_lines_kernel<512><<<(int)lines, 512, 0, st>>>(a);
+    else compact_lines_kernel<1024><<<(int)lines, 1024, 0, st>>>(a);
     BASA_HIP_CHECK_LAUNCH("compact_lines_kernel");
   }
   return BASA_OK;

@@ -79,6 +79,16 @@ def test_long_contexts_of_which_tokens_are_dropped(dtype, d, heads, page, layout
     _compact_check(dtype, d, heads, page, layout, [0, 0, 4, 3, 0, 0], kept, 7)
 
 
+# both sides of where lists are long: 48 moves and one for every 48 lines of 128 bytes; of 200 sequences short lists go past a block of moves
+@pytest.mark.parametrize("dtype,d,n,most", [(BF, 64, 1, 48), (BF, 64, 1, 49), (BF, 128, 8, 53), (BF, 128, 8, 54), (BF, 128, 64, 90), (BF, 128, 64, 91), (F32, 128, 200, 314),
+                                            (F32, 128, 200, 315), (BF, 128, 16, 600), (BF, 128, 15, 600)])
+def test_short_and_long_lists(dtype, d, n, most):
+    rng = np.random.default_rng(n + most)
+    kept = [subset(int(rng.integers(1, 2 * most)), 0.5, rng) for _ in range(n)]
+    kept[n // 2] = subset(most + most // 3, 1.0, rng)[most // 3:][:most]
+    _compact_check(dtype, d, 8, 16, "head", rng.integers(0, 40, n).tolist(), kept, n)
+
+
 def test_one_long_context():
     rng = np.random.default_rng(1)
     for share in (0.3, 0.999):
