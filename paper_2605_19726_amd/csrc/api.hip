@@ -925,7 +925,7 @@ basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_
   if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
   if (most < 0 || keep_stride < most) { set_error("rows of keep are %lld entries apart, %d wide", (long long)keep_stride, most); return BASA_ERR_INVALID_ARG; }
   if (n_seq > 0 && most > 0 && (!start || !keep || !count)) { set_error("null start, keep or count"); return BASA_ERR_INVALID_ARG; }
-  if (!compact_takes(n_seq, view_of(*k_pages), most)) {
+  if (!compact_takes(n_seq, view_of(*k_pages))) {
     set_error("%d sequences of %d heads: more than a call takes", n_seq, k_pages->heads); return BASA_ERR_UNSUPPORTED;
   }
   return launch_cache_compact(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, start, keep, most, keep_stride, count, n_seq,

@@ -4,6 +4,19 @@
 // every token before base, and new token j if bit j of its mask is set (a chain: j <= t).  Rows of a KV head: (t, h), n x group of them.  For
 // a row:  s_j = q . k_j,  m = max s_j,  o = sum_j e^((s_j - m) / sqrt(d)) v_j / sum_j e^((s_j - m) / sqrt(d)),  lse = m / sqrt(d) + ln sum, over the tokens
 // that it sees.  One pass over the tokens with a running maximum and sum per row.
+//
+// Bound by the memory up to some 64 rows of a KV head (bf16), by the matrix and vector units and the card's power from 200 on.  What carries it:
+//   - All rows of a KV head share a token's K and V: a workgroup has a tile of 32 to 256 of them, a wave 32 (f32: 16), and the tokens come by in steps of 32 (16) through a
+//     ring in the LDS, which requests to memory fill without registers (32 sequences of 1000 to 16000 tokens, 8 to 24 new ones, 32 heads on 8, d = 128: 698 MB in 144 us,
+//     4.85 TB/s; 16 rows to a wave, its operands from memory: 180).
+//   - S^T = K Q^T and O^T = V^T P^T: a lane has the same row in the scores, the weights and the output, so that weights are operands where they are, and the maximum and
+//     the sum of a row are two lanes' (four).
+//   - Weights enter the second product as two bf16 numbers, the upper half of the f32 and the rest: three products of matrix units for two of the formula, and the only rounding to
+//     8 bits is the output's.  (131072 tokens, 64 new ones, 256 rows: 229 us, 911 TF executed of the 1276 that a large product of matrices runs at.  Half of the cycles
+//     the matrix units work, and half the vector units; to have them overlap more, by the next step's scores during this one's products, by waves of different
+//     priority, by one barrier to two or four steps, leaves the time as it is (225 to 240): the clock falls to 1.8 GHz.)
+//   - Work is cut on one axis (paged_plan.hpp): KV head by KV head, in each the sequences, in each the tiles of rows, each with a place for every step and some for what a
+//     piece costs by itself; every workgroup finds its run of places from the lengths.  Pieces are added up by a second kernel where their L2 has them.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -93,11 +106,10 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
   }
 }
 // 16 bytes from memory for every lane, side by side into the LDS.  Written in assembly, without a register for its result: the compiler would wait for all of
-// these before it reads the LDS or meets a barrier; the waits stand where the ring needs them.
-template <bool kOnce>
+// these before it reads the LDS or meets a barrier; the waits stand where the ring needs them.  As a stream that no cache keeps: 8 new tokens of 32 sequences 130 us, and 148
+// without that; level where a KV head has several tiles and reads its rows as often.
 __device__ __forceinline__ void to_lds(const char* from, uint32_t at) {
-  if constexpr (kOnce) asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(at) : "memory");
-  else asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "s"(at) : "memory");
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(at) : "memory");
 }
 __device__ __forceinline__ void word_to_lds(const void* from, uint32_t at) {      // 4 bytes for every lane
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at) : "memory");
@@ -471,7 +483,7 @@ __device__ __forceinline__ void wait_for_all_but(int steps) {
   else if constexpr (kMost > 0) wait_for_all_but<kMost - 1, kLoads>(steps);
 }
 
-template <bool kBf16, int kD, int kWaves, bool kSplit, bool kOnce>
+template <bool kBf16, int kD, int kWaves, bool kSplit>
 __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::kWavesPerSimd)) void tree_kernel(TreeArgs a) {
   using G = Geometry<kBf16, kD, kWaves, kSplit>;
   using R = Rows<kBf16, kD>;
@@ -619,7 +631,7 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
 #pragma unroll
       for (int i = 0; i < G::kLoads; ++i) {
         const uint2 at = places_at[(step * G::kStep + from_row[i]) & (2 * kWindow - 1)];
-        to_lds<kOnce>(from[i] + ((uint64_t)(from_v[i] ? at.y : at.x) << a.unit), ring + stage * G::kStageBytes + (i * kWaves + wave) * 1024);
+        to_lds(from[i] + ((uint64_t)(from_v[i] ? at.y : at.x) << a.unit), ring + stage * G::kStageBytes + (i * kWaves + wave) * 1024);
       }
     };
     // Every step in turn: body(step, place of its K in the LDS, next), which has everyone call next() once.
@@ -738,7 +750,7 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
   }
 }
 
-// First places of many sequences: one workgroup, a run of sequences to a thread.
+// First places of many sequences: one workgroup, a run of sequences to a thread.  (Up to kPlanBatch a launch less: 64 sequences 12.1 us in all.)
 __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs a, int step, int tile, bool split) {
   __shared__ int wave_sum[16];
   const int tid = threadIdx.x, each = (a.n + 1023) / 1024, i0 = min(tid * each, a.n), i1 = min(i0 + each, a.n);
@@ -869,7 +881,7 @@ TreeWs carve(int n, int64_t rows, int64_t runs, int tile, int d) {
 template <bool kBf16, int kD, int kWaves, bool kSplit>
 basa_status launch_kernel(const TreeArgs& a, hipStream_t st) {
   using G = Geometry<kBf16, kD, kWaves, kSplit>;
-  const auto kernel = tree_kernel<kBf16, kD, kWaves, kSplit, true>;
+  const auto kernel = tree_kernel<kBf16, kD, kWaves, kSplit>;
   if (a.n > kPlanBatch) {
     ProfScope prof(K_TREE, st);
     tree_plan_kernel<<<1, 1024, 0, st>>>(a, G::kStep, G::kRowTile, kSplit);

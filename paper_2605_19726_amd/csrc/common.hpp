@@ -201,7 +201,7 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
 constexpr int kMaxMaskWords = 64;
 basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, int tokens, int64_t* masks, int words, int64_t mask_stride,
                               int32_t* depths, hipStream_t st);
-bool compact_takes(int n, const TensorView& k_pages, int most);
+bool compact_takes(int n, const TensorView& k_pages);
 basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
                                  const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
                                  hipStream_t st);

@@ -484,10 +484,8 @@ basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, 
 }
 
 // A launch has less than 2^32 threads.
-bool compact_takes(int n, const TensorView& k, int most) {
-  const int64_t row_lines = k.d * (k.dtype == BASA_BF16 ? 2 : 4) / kLine;
-  const int64_t lines = n * row_lines * k.heads * 2;
-  return n <= 1 << 22 && (is_short(most, lines) || lines < (1 << 23));
+bool compact_takes(int n, const TensorView& k) {
+  return n <= 1 << 22 && (int64_t)n * k.heads * (k.d * (k.dtype == BASA_BF16 ? 2 : 4) / kLine) * 2 < (1 << 23);
 }
 basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
                                  const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
