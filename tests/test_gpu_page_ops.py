@@ -178,6 +178,26 @@ def test_copies_of_pages(dtype, d, heads, page, layout):
     bd.basa_cache_copy(bd.PagedCache(k, v), ints(np.zeros((0, 3))))
 
 
+# pages, or heads, more than 4 GiB apart in all
+@pytest.mark.parametrize("strides", [(2 ** 28 + 8, 1000, 2 ** 15 + 24), (2 ** 13, 2 ** 31 + 64, 136)])
+def test_moves_and_copies_of_pages_beyond_32_bits(strides):
+    rng = np.random.default_rng(5)
+    small = [filled(20, 3, 16, 64, BF, "head", i) for i in range(2)]
+    size = sum((n - 1) * x for n, x in zip((20, 3, 16), strides)) + 64
+    k, v = (torch.empty(size, dtype=BF, device=DEV).as_strided(x.shape, (*strides, 1)).copy_(x) for x in small)
+    table = rng.permutation(20)[:18].reshape(2, 9).astype(np.int32)
+    for most in (20, 100):
+        keep = np.array([np.sort(rng.permutation(140)[:most]) for _ in range(2)], dtype=np.int32)
+        moves = compact(table, [2, 0], keep, [most, most - 1], 16, 20)
+        small = [moved(x, moves).view(20, 16, 3, 64).permute(0, 2, 1, 3) for x in small]
+        bd.basa_cache_compact(bd.PagedCache(k, v), ints(table), ints([2, 0]), ints(keep), ints([most, most - 1]))
+        assert all(torch.equal(bits(x.contiguous()), bits(y.contiguous())) for x, y in zip(small, (k, v)))
+    bd.basa_cache_copy(bd.PagedCache(k, v), ints([[0, 19, 7], [18, 1, 16]]))
+    for x in small:
+        x[19, :, :7], x[1] = x[0, :, :7].clone(), x[18].clone()
+    assert all(torch.equal(bits(x.contiguous()), bits(y.contiguous())) for x, y in zip(small, (k, v)))
+
+
 # ---------------------------------------------------------------- free pages
 def _free_check(table, lens, page, pages):
     want = free_pages(table, lens, page, pages)

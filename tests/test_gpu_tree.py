@@ -286,6 +286,24 @@ def test_offsets_that_do_not_ascend_stay_in_bounds():
             torch.cuda.synchronize()
 
 
+def _spread(x, stride_b, stride_h, stride_l):
+    """The same pages far apart, in storage of which nothing else is ever written."""
+    n, h, t, d = x.shape
+    size = (n - 1) * stride_b + (h - 1) * stride_h + (t - 1) * stride_l + d
+    y = torch.empty(size, dtype=x.dtype, device=DEV).as_strided(x.shape, (stride_b, stride_h, stride_l, 1))
+    return y.copy_(x)
+
+
+# pages, or heads, more than 4 GiB apart in all; strides that only 16 bytes divide
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("stride_b,stride_h,stride_l", [(2 ** 27 + 8, 1000, 2 ** 15 + 24), (2 ** 13, 2 ** 31 + 64, 136), (2 ** 27, 2 ** 20, 256)])
+def test_offsets_beyond_32_bits(dtype, d, stride_b, stride_h, stride_l):
+    c = Case(dtype, d, 8, 2, 16, [300, 17, 120], [20, 3, 70], 13)
+    assert c.k.shape[0] > 30
+    c.k, c.v = _spread(c.k, stride_b, stride_h, stride_l), _spread(c.v, stride_b, stride_h, stride_l)
+    c.check(*c.run(), f"{dtype} {stride_b} {stride_h}")
+
+
 def test_no_tokens_or_no_sequences_is_no_work():
     cache = bd.PagedCache(*(store(2, 2, 16, 64, BF, "head", DEV, 1.0) for _ in range(2)))
     none = torch.empty(0, 4, 64, dtype=BF, device=DEV)
