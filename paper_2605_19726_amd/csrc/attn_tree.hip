@@ -300,6 +300,12 @@ struct Rows<true, kD> {
 #pragma unroll
       for (int i = 0; i < 16; i += 4) f(32 * e + 2 * i + 4 * (lane >> 5), floatx4{acc[e][i], acc[e][i + 1], acc[e][i + 2], acc[e][i + 3]});
   }
+  static constexpr int kQuads = 4 * kBlocks;    // of a lane's sums
+  __device__ __forceinline__ floatx4 quad(int i) const { return {acc[i / 4][4 * (i & 3)], acc[i / 4][4 * (i & 3) + 1], acc[i / 4][4 * (i & 3) + 2], acc[i / 4][4 * (i & 3) + 3]}; }
+  __device__ __forceinline__ void set_quad(int i, floatx4 x) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc[i / 4][4 * (i & 3) + j] = x[j];
+  }
   // The row divided by its sum: lanes h and 32 + h have four dimensions each of the same eight, and exchange them for eight each of sixteen.
   __device__ __forceinline__ void store(char* to, float sum, int lane, bool mine) const {
     const float by = 1.0f / sum;
@@ -453,6 +459,9 @@ struct Rows<false, kD> {
       for (int x = 0; x < kD / 64; ++x)
         f(64 * x + 4 * (4 * (lane >> 4) + i), floatx4{acc[4 * x][i], acc[4 * x + 1][i], acc[4 * x + 2][i], acc[4 * x + 3][i]});
   }
+  static constexpr int kQuads = kBlocks;
+  __device__ __forceinline__ floatx4 quad(int i) const { return acc[i]; }
+  __device__ __forceinline__ void set_quad(int i, floatx4 x) { acc[i] = x; }
   __device__ __forceinline__ void store(char* to, float sum, int lane, bool mine) const {
     each(lane, [&](int dim, floatx4 o) { if (mine) *reinterpret_cast<floatx4*>(to + dim * 4) = normalised(o, sum); });
   }
@@ -470,10 +479,13 @@ struct Geometry {
   static constexpr bool kLarge = kStageBytes > 8 * 1024;
   static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? (kLarge ? 4 : 8) : kLarge && !kSplit ? 2 : 4;
   static constexpr int kGroups = kWaves == 8 ? 1 : kWaves == 4 ? 2 : kLarge && kSplit ? 2 : 4;         // workgroups that a compute unit holds
+  static constexpr int kMostWays = kWaves == 8 || kStages < 4 ? 1 : 2;
+  static constexpr int kStateBytes = R::kQuads * 1024 + 512;   // what a wave hands over
   static constexpr int kWavesPerSimd = (kGroups * kWaves + 3) / 4;
   static constexpr int kPlacesAt = kStages * kStageBytes, kIdsAt = kPlacesAt + 2 * kWindow * 8;       // places of K and V, page ids
   static constexpr int kLiveAt = kIdsAt + 2 * kWindow * 4, kVoteAt = kLiveAt + 2 * kWindow / 8, kLdsBytes = kVoteAt + 16;
   static_assert(kGroups * kLdsBytes <= 160 * 1024, "the LDS");
+  static_assert((kWaves - 1) * kStateBytes <= kPlacesAt && (kStages & (kStages - 1)) == 0, "the ring");
 };
 
 // All but the youngest `steps` requests of a wave have landed, of kLoads each; more than kMost are not waited for.
@@ -580,172 +592,207 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
 
     R rw;
     const uint32_t ring = lds_address(smem), k_lane = R::k_at(lane), v_lane = R::v_at(lane);
-    const int row_first = wave * R::kRows;        // of the unit
-    const bool works = row_first < unit_rows;
-    const int my_row = unit * G::kRowTile + min(row_first + R::column(lane), unit_rows - 1);
-    const int my_token = (int)a.per_token.div(my_row), my_head = kvh * a.group + my_row - my_token * a.group;
-    const int32_t* const table = a.table + (int64_t)seq_b * a.table_stride;
-    const char* const k_head = a.k + kvh * a.k_h;
-    const char* const v_head = a.v + kvh * a.v_h;
-    // Page ids of a window of tokens, on their way to the LDS like everything else; then their tokens' places.
-    auto fetch_ids = [&](int window) {
-      const int tok0 = window * kWindow, p0 = (int)a.page.div(min(tok0, limit - 1)), last = (int)a.page.div(limit - 1);
-      for (int i = wave; i < kWindow / 64; i += kWaves)
-        word_to_lds(table + min(p0 + 64 * i + lane, last), ring + G::kIdsAt + ((window & 1) * kWindow + 64 * i) * 4);
-    };
-    const int window0 = t0 * G::kStep / kWindow;
-    if (t0 < t1) {
-      fetch_ids(window0);
-      fetch_ids(window0 + 1);
-    }
-    rw.load_q(a.q + (seq.row0 + my_token) * a.q_t + my_head * a.q_h, lane);
-    // the first two words of the row's mask, all of them as a rule
-    const uint64_t* const my_mask = a.masks ? a.masks + (seq.row0 + my_token) * a.mask_stride : nullptr;
-    const uint64_t mask0 = a.masks ? my_mask[0] : 0, mask1 = a.masks && a.words > 1 ? my_mask[1] : 0;
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0), for the compiler to know: it would wait for the queries in the loop, and for the ring with them
-    auto place_tokens = [&](int window) {         // everyone is there before and after
-      const int side = window & 1, tok0 = window * kWindow, p0 = (int)a.page.div(tok0);
-#pragma unroll
-      for (int at = tid; at < kWindow; at += kThreads) {
-        const int tok = min(tok0 + at, limit - 1), p = (int)a.page.div(tok), off = tok - p * (int)a.page.d;      // (behind the last: that one's place again)
-        const uint32_t id = ids[side * kWindow + p - p0];
-        const bool held = id < (uint32_t)a.pages;
-        places_at[side * kWindow + at] = held ? make_uint2(id * a.k_b + off * a.k_l, id * a.v_b + off * a.v_l) : make_uint2(0u, 0u);
-        const uint64_t live = __ballot(held && tok0 + at < limit);
-        if (lane == 0) live_at[(side * kWindow + at) >> 6] = live;
+    // Of few rows half of the waves have no work; they take every second step of the same rows then, two steps to a barrier, and hand their sums over in the end.  A wave alone
+    // takes longer for a step than memory does: 16 rows of 16 sequences of 4000, f32, d = 128, 120 -> 99 us; 64 of 32 of 1000 to 16000, bf16, 154 -> 142.  Four steps side by
+    // side, of eight waves, are slower (168 and 155 us of 32 to 96 rows): too few are on their way.
+    const int needed = unit_rows > 4 * R::kRows ? 8 : unit_rows > 2 * R::kRows ? 4 : unit_rows > R::kRows ? 2 : 1;
+    const int way = wave / needed;
+    auto attend = [&](auto constant) {
+      constexpr int ways = decltype(constant)::value;
+      const int row_first = (wave & (needed - 1)) * R::kRows;        // of the unit
+      const bool works = row_first < unit_rows && way < ways;
+      const int my_row = unit * G::kRowTile + min(row_first + R::column(lane), unit_rows - 1);
+      const int my_token = (int)a.per_token.div(my_row), my_head = kvh * a.group + my_row - my_token * a.group;
+      const int32_t* const table = a.table + (int64_t)seq_b * a.table_stride;
+      const char* const k_head = a.k + kvh * a.k_h;
+      const char* const v_head = a.v + kvh * a.v_h;
+      // Page ids of a window of tokens, on their way to the LDS like everything else; then their tokens' places.
+      auto fetch_ids = [&](int window) {
+        const int tok0 = window * kWindow, p0 = (int)a.page.div(min(tok0, limit - 1)), last = (int)a.page.div(limit - 1);
+        for (int i = wave; i < kWindow / 64; i += kWaves)
+          word_to_lds(table + min(p0 + 64 * i + lane, last), ring + G::kIdsAt + ((window & 1) * kWindow + 64 * i) * 4);
+      };
+      const int window0 = t0 * G::kStep / kWindow;
+      if (t0 < t1) {
+        fetch_ids(window0);
+        fetch_ids(window0 + 1);
       }
-    };
-    // What a lane fetches of a step: 16 bytes of K or V of a token in each of its wave's requests.
-    const char* from[G::kLoads];
-    int from_row[G::kLoads];
-    bool from_v[G::kLoads];
+      rw.load_q(a.q + (seq.row0 + my_token) * a.q_t + my_head * a.q_h, lane);
+      // the first two words of the row's mask, all of them as a rule
+      const uint64_t* const my_mask = a.masks ? a.masks + (seq.row0 + my_token) * a.mask_stride : nullptr;
+      const uint64_t mask0 = a.masks ? my_mask[0] : 0, mask1 = a.masks && a.words > 1 ? my_mask[1] : 0;
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_s_waitcnt(0x0f70);           // vmcnt(0), for the compiler to know: it would wait for the queries in the loop, and for the ring with them
+      auto place_tokens = [&](int window) {         // everyone is there before and after
+        const int side = window & 1, tok0 = window * kWindow, p0 = (int)a.page.div(tok0);
 #pragma unroll
-    for (int i = 0; i < G::kLoads; ++i) {
-      const int chunk = i * kWaves + wave, in_half = chunk % (G::kHalfBytes / 1024), c = lane % R::kChunks;
-      from_row[i] = in_half * (1024 / R::kRowBytes) + lane / R::kChunks;
-      from_v[i] = chunk >= G::kHalfBytes / 1024;
-      from[i] = from_v[i] ? v_head + R::v_place(from_row[i], c) * 16 : k_head + R::k_place(from_row[i], c) * 16;
-    }
-    auto issue = [&](int step, int stage) {
+        for (int at = tid; at < kWindow; at += kThreads) {
+          const int tok = min(tok0 + at, limit - 1), p = (int)a.page.div(tok), off = tok - p * (int)a.page.d;      // (behind the last: that one's place again)
+          const uint32_t id = ids[side * kWindow + p - p0];
+          const bool held = id < (uint32_t)a.pages;
+          places_at[side * kWindow + at] = held ? make_uint2(id * a.k_b + off * a.k_l, id * a.v_b + off * a.v_l) : make_uint2(0u, 0u);
+          const uint64_t live = __ballot(held && tok0 + at < limit);
+          if (lane == 0) live_at[(side * kWindow + at) >> 6] = live;
+        }
+      };
+      // What a lane fetches of a step: 16 bytes of K or V of a token in each of its wave's requests.
+      const char* from[G::kLoads];
+      int from_row[G::kLoads];
+      bool from_v[G::kLoads];
 #pragma unroll
       for (int i = 0; i < G::kLoads; ++i) {
-        const uint2 at = places_at[(step * G::kStep + from_row[i]) & (2 * kWindow - 1)];
-        to_lds(from[i] + ((uint64_t)(from_v[i] ? at.y : at.x) << a.unit), ring + stage * G::kStageBytes + (i * kWaves + wave) * 1024);
+        const int chunk = i * kWaves + wave, in_half = chunk % (G::kHalfBytes / 1024), c = lane % R::kChunks;
+        from_row[i] = in_half * (1024 / R::kRowBytes) + lane / R::kChunks;
+        from_v[i] = chunk >= G::kHalfBytes / 1024;
+        from[i] = from_v[i] ? v_head + R::v_place(from_row[i], c) * 16 : k_head + R::k_place(from_row[i], c) * 16;
       }
-    };
-    // Every step in turn: body(step, place of its K in the LDS, next), which has everyone call next() once.
-    bool again = false;
-    auto traverse = [&](auto body) {
-      int placed = window0;                       // the last window whose tokens' places are there
-      int stage_to = 0, stage_at = 0;
-      if (t0 < t1) {
-        if (again) {
-          fetch_ids(placed);
-          fetch_ids(placed + 1);
-          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      auto issue = [&](int step, int stage) {
+#pragma unroll
+        for (int i = 0; i < G::kLoads; ++i) {
+          const uint2 at = places_at[(step * G::kStep + from_row[i]) & (2 * kWindow - 1)];
+          to_lds(from[i] + ((uint64_t)(from_v[i] ? at.y : at.x) << a.unit), ring + stage * G::kStageBytes + (i * kWaves + wave) * 1024);
         }
-        again = true;
-        meet();
-        place_tokens(placed);
-        meet();
-      }
-      auto request = [&](int step) {              // (uniform, and so are the barriers in it)
-        if (step >= t1) return;
-        if (step * G::kStep / kWindow != placed) {        // its ids were asked for a window ago, and have landed with the step that everyone has waited for
-          ++placed;
+      };
+      // Steps in turn, `ways` at a time: body(the first, next), which has everyone call next() once.
+      auto stage_of = [&](int step) { return ring + ((step - t0) & (G::kStages - 1)) * G::kStageBytes; };
+      bool again = false;
+      auto traverse = [&](auto body) {
+        int placed = window0;                       // the last window whose tokens' places are there
+        if (t0 < t1) {
+          if (again) {
+            fetch_ids(placed);
+            fetch_ids(placed + 1);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          }
+          again = true;
+          meet();
           place_tokens(placed);
           meet();
-          fetch_ids(placed + 1);
         }
-        issue(step, stage_to);
-        stage_to = stage_to + 1 == G::kStages ? 0 : stage_to + 1;
-      };
-      static_assert(kWindow / G::kStep >= G::kStages, "page ids that have landed, places that no one reads any more");
-#pragma clang loop unroll(disable)
-      for (int i = 0; i < G::kStages - 1; ++i) request(t0 + i);
-#pragma clang loop unroll(disable)
-      for (int t = t0; t < t1; ++t) {
-        // all but my youngest requests have landed; after the barrier everyone's have, and everyone is done with the step before
-        wait_for_all_but<G::kStages - 2, G::kLoads>(t1 - 1 - t);
-        meet();
-        body(t, ring + stage_at * G::kStageBytes, [&] { request(t + G::kStages - 1); });
-        stage_at = stage_at + 1 == G::kStages ? 0 : stage_at + 1;
-      }
-      meet();
-    };
-    auto seen_of = [&](int t) {                   // of the wave's tokens: whether there are any that the lane's row does not see, and which it does
-      const int tok0 = t * G::kStep, at = tok0 - base;         // `at`: of the first token among the new ones
-      constexpr uint32_t kAll = ~0u >> (32 - G::kStep);
-      const uint32_t live = __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t*>(live_at)[(tok0 & (2 * kWindow - 1)) >> 5] >> (tok0 & 31)) & kAll;
-      Seen s{at > -G::kStep || live != kAll, kAll};
-      if (s.masked) {
-        s.bits = chain_bits(my_token, at);
-        if (my_mask) {
-          const int w = max(at, 0) >> 6;
-          if (w == 0) s.bits = tree_bits(mask0, mask1, at);
-          else s.bits = tree_bits(w == 1 ? mask1 : w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
-        }
-        s.bits &= live;
-      }
-      return s;
-    };
-    // Once as it is.  A weight of zero, or a part of one that is, times infinity or NaN is NaN, also where a row does not see the token: if there is NaN in the result
-    // of a workgroup, once more with the values that are finite, and then the others added to the rows that see them.
-    bool clean = false;
-#pragma clang loop unroll(disable)
-    for (;;) {
-      rw.clear();
-      traverse([&](int t, uint32_t k_stage, auto next) {
-        if (clean) {
-          for (int i = tid; i < G::kHalfBytes / 16; i += kThreads) {
-            const lds_chunk_ptr_t at = (lds_chunk_ptr_t)(uintptr_t)(k_stage + G::kHalfBytes + i * 16);
-            *at = R::finite(*at);
+        auto request = [&](int step) {              // (uniform, and so are the barriers in it)
+          if (step >= t1) return;
+          if (step * G::kStep / kWindow != placed) {        // its ids were asked for a window ago, and have landed with the step that everyone has waited for
+            ++placed;
+            place_tokens(placed);
+            meet();
+            fetch_ids(placed + 1);
           }
-          meet();
-        }
-        if (!works) {
-          next();
-          return;
-        }
-        rw.step(k_stage + k_lane, k_stage + G::kHalfBytes + v_lane, a.scale_log2e, lane, [&] {
-          const Seen seen = seen_of(t);
-          next();
-          return seen;
-        });
-      });
-      if (clean) break;
-      if (tid == 0) *vote = 0;
-      meet();
-      if (works && rw.any_nan() && lane == 0) *vote = 1;
-      meet();
-      if (!*vote) break;
-      clean = true;
-    }
-    if (clean) {
-      traverse([&](int t, uint32_t k_stage, auto next) {
-        next();
-        if (!works) return;
-        const Seen seen = seen_of(t);
-        const uint32_t on = rw.weighs(k_stage + k_lane, seen, a.scale_log2e, lane);
+          issue(step, (step - t0) & (G::kStages - 1));
+        };
+        static_assert(kWindow / G::kStep >= G::kStages, "page ids that have landed, places that no one reads any more");
 #pragma clang loop unroll(disable)
-        for (int i = 0; i < G::kStep; ++i) rw.add_not_finite(k_stage + G::kHalfBytes, i, seen.bits >> i & 1, on >> i & 1, lane);
-      });
-    }
+        for (int i = 0; i < G::kStages - ways; ++i) request(t0 + i);
+#pragma clang loop unroll(disable)
+        for (int t = t0; t < t1; t += ways) {
+          // all but my youngest requests have landed; after the barrier everyone's have, and everyone is done with the steps before
+          wait_for_all_but<G::kStages - 2, G::kLoads>(min(G::kStages - 2 * ways, max(t1 - ways - t, 0)));
+          meet();
+          body(t, [&] {
+#pragma clang loop unroll(disable)
+            for (int i = 0; i < ways; ++i) request(t + G::kStages - ways + i);
+          });
+        }
+        meet();
+      };
+      auto seen_of = [&](int t) {                   // of the wave's tokens: whether there are any that the lane's row does not see, and which it does
+        const int tok0 = t * G::kStep, at = tok0 - base;         // `at`: of the first token among the new ones
+        constexpr uint32_t kAll = ~0u >> (32 - G::kStep);
+        const uint32_t live = __builtin_amdgcn_readfirstlane(reinterpret_cast<const uint32_t*>(live_at)[(tok0 & (2 * kWindow - 1)) >> 5] >> (tok0 & 31)) & kAll;
+        Seen s{at > -G::kStep || live != kAll, kAll};
+        if (s.masked) {
+          s.bits = chain_bits(my_token, at);
+          if (my_mask) {
+            const int w = max(at, 0) >> 6;
+            if (w == 0) s.bits = tree_bits(mask0, mask1, at);
+            else s.bits = tree_bits(w == 1 ? mask1 : w < a.words ? my_mask[w] : 0, w + 1 < a.words ? my_mask[w + 1] : 0, at);
+          }
+          s.bits &= live;
+        }
+        return s;
+      };
+      // Once as it is.  A weight of zero, or a part of one that is, times infinity or NaN is NaN, also where a row does not see the token: if there is NaN in the result
+      // of a workgroup, once more with the values that are finite, and then the others added to the rows that see them.
+      bool clean = false;
+#pragma clang loop unroll(disable)
+      for (;;) {
+        rw.clear();
+        traverse([&](int t, auto next) {
+          if (clean) {
+            for (int step = t; step < min(t + ways, t1); ++step)
+              for (int i = tid; i < G::kHalfBytes / 16; i += kThreads) {
+                const lds_chunk_ptr_t at = (lds_chunk_ptr_t)(uintptr_t)(stage_of(step) + G::kHalfBytes + i * 16);
+                *at = R::finite(*at);
+              }
+            meet();
+          }
+          if (!works || t + way >= t1) {
+            next();
+            return;
+          }
+          const uint32_t stage = stage_of(t + way);
+          rw.step(stage + k_lane, stage + G::kHalfBytes + v_lane, a.scale_log2e, lane, [&] {
+            const Seen seen = seen_of(t + way);
+            next();
+            return seen;
+          });
+        });
+        if (clean) break;
+        if (tid == 0) *vote = 0;
+        meet();
+        if (works && rw.any_nan() && lane == 0) *vote = 1;
+        meet();
+        if (!*vote) break;
+        clean = true;
+      }
+      if (clean) {
+        traverse([&](int t, auto next) {
+          next();
+          if (!works || t + way >= t1) return;
+          const Seen seen = seen_of(t + way);
+          const uint32_t stage = stage_of(t + way), on = rw.weighs(stage + k_lane, seen, a.scale_log2e, lane);
+#pragma clang loop unroll(disable)
+          for (int i = 0; i < G::kStep; ++i) rw.add_not_finite(stage + G::kHalfBytes, i, seen.bits >> i & 1, on >> i & 1, lane);
+        });
+      }
+      if constexpr (ways > 1) {                     // the ring is free
+        auto state_of = [&](int from) { return smem + (from - needed) * G::kStateBytes; };
+        if (works && way > 0) {
+          char* const to = state_of(wave);
+#pragma unroll
+          for (int i = 0; i < R::kQuads; ++i) *reinterpret_cast<floatx4*>(to + (i * 64 + lane) * 16) = rw.quad(i);
+          *reinterpret_cast<float2*>(to + R::kQuads * 1024 + lane * 8) = make_float2(rw.m, rw.l);
+        }
+        meet();
+        if (works && way == 0)
+#pragma clang loop unroll(disable)
+          for (int w = 1; w < ways; ++w) {
+            const char* const from = state_of(wave + w * needed);
+            const float2 ml = *reinterpret_cast<const float2*>(from + R::kQuads * 1024 + lane * 8);
+            const float top = fmaxf(rw.m, ml.x), f = factor_of(rw.m, top), x = factor_of(ml.x, top);
+            rw.m = top;
+            rw.l = rw.l * f + ml.y * x;
+#pragma unroll
+            for (int i = 0; i < R::kQuads; ++i) rw.set_quad(i, rw.quad(i) * f + *reinterpret_cast<const floatx4*>(from + (i * 64 + lane) * 16) * x);
+          }
+      }
 
-    const float sum = rw.whole_sum();
-    const int row = row_first + R::column(lane);  // of the unit
-    const bool there = row < unit_rows;
-    const int64_t id = (int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head;
-    if (kSplit && has_first && there && R::writes_sum(lane)) a.cut_of[id] = whole ? -1 : pack_cut(group, last, row);
-    if (whole) {
-      rw.store(a.out + (seq.row0 + my_token) * a.out_t + my_head * a.out_h, sum, lane, there);
-      if (a.lse && there && R::writes_sum(lane)) a.lse[id] = lse_of(rw.m, sum);
-    } else if (there) {
-      const int64_t to = (int64_t)place * G::kRowTile + row;
-      rw.each(lane, [&](int dim, floatx4 o) { *reinterpret_cast<floatx4*>(a.part_o + to * kD + dim) = o; });
-      if (R::writes_sum(lane)) a.part_ml[to] = make_float2(rw.m, sum);
-    }
+      const float sum = rw.whole_sum();
+      const int row = row_first + R::column(lane);  // of the unit
+      const bool there = row < unit_rows && way == 0;
+      const int64_t id = (int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head;
+      if (kSplit && has_first && there && R::writes_sum(lane)) a.cut_of[id] = whole ? -1 : pack_cut(group, last, row);
+      if (whole) {
+        rw.store(a.out + (seq.row0 + my_token) * a.out_t + my_head * a.out_h, sum, lane, there);
+        if (a.lse && there && R::writes_sum(lane)) a.lse[id] = lse_of(rw.m, sum);
+      } else if (there) {
+        const int64_t to = (int64_t)place * G::kRowTile + row;
+        rw.each(lane, [&](int dim, floatx4 o) { *reinterpret_cast<floatx4*>(a.part_o + to * kD + dim) = o; });
+        if (R::writes_sum(lane)) a.part_ml[to] = make_float2(rw.m, sum);
+      }
+    };
+    const int most_ways = min(kWaves / needed, G::kMostWays);     // (constants, for the loops of one step at a time: 3% of large trees)
+    if (most_ways <= 1) attend(std::integral_constant<int, 1>{});
+    else if constexpr (G::kMostWays > 1) attend(std::integral_constant<int, 2>{});
     if constexpr (kSplit) meet();
   }
 }

@@ -252,6 +252,38 @@ def test_infinite_values_stay_infinite():
         assert torch.isfinite(out[int(c.cu[1]):int(c.cu[2])].float()).all()
 
 
+# few rows: waves take steps of the same rows side by side, and what is not finite stands in the steps of either
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("lens", [[300, 40], [5000, 95], [31, 33]])
+def test_values_that_are_not_finite_of_few_rows(dtype, d, lens):
+    c = Case(dtype, d, 4, 2, 16, lens, [5, 7], 6, q_scale=0.5)
+    out, lse = c.run()
+    c.check(out, lse)
+    for i, n in enumerate(lens):
+        at, off = (x.to(DEV) for x in rows_of(c.table[i], n, 16))
+        a, m = int(c.cu[i]), c.new[i]
+        k, v = c.k.clone(), c.v.clone()
+        for t in (0, 16, 33, 65, n - m):                        # of the context: every row; the first new one: those that follow it
+            if t >= n:
+                continue
+            c.v[at[t], 1, off[t], 3] = INF
+            got, _ = c.run()
+            rows = got[a:a + m].float()
+            sees = torch.from_numpy(c.seen[i][:, t - (n - m)]).to(DEV) if t >= n - m else torch.ones(m, dtype=torch.bool, device=DEV)
+            assert (rows[sees][:, 2:, 3] == INF).all() and torch.isfinite(rows[~sees]).all()
+            assert torch.equal(bits(got[a:a + m, :2]), bits(out[a:a + m, :2]))                     # the other KV head
+            others = [x for x in range(d) if x != 3]
+            assert (rows[:, :, others] - out[a:a + m].float()[:, :, others]).abs().max() <= 2.0 ** -6 * c.v[at, :, off].float().nan_to_num(0, 0, 0).abs().max()
+            c.v.copy_(v)
+        leaf = n - 1                                            # seen by itself alone
+        c.k[at[leaf], :, off[leaf]], c.v[at[leaf], :, off[leaf]] = NAN, NAN
+        got, _ = c.run()
+        check_tree(got, None, c.q, c.k, c.v, c.table, c.lens, c.cu, c.seen, f"{dtype} {d} {lens}", only=(i, list(range(m - 1))))
+        assert torch.isnan(got[a + m - 1].float()).all()
+        c.k.copy_(k)
+        c.v.copy_(v)
+
+
 def test_scores_that_are_minus_infinity():
     for dtype in (BF, F32):
         c = Case(dtype, 64, 2, 1, 16, [50], [4], 3, around=(0, 0))
