@@ -467,7 +467,7 @@ struct Rows<false, kD> {
   }
 };
 
-// A workgroup has a wave for every kRows rows of a tile; each takes every token.  Of a ring of kStages steps in the LDS one is worked on, the others are on
+// A workgroup has a wave for every kRows rows of a tile; each takes every token (every second step, where two waves share rows).  Of a ring of kStages steps in the LDS one is worked on, the others are on
 // their way there: 64 KB for a workgroup of two or four waves, two to a compute unit, 128 KB for one of eight.  Short sequences of few rows want more workgroups, not more
 // steps ahead: two steps in the ring and four workgroups (64 sequences of 60 tokens, bf16, d = 128: 16.4 -> 12.1 us; 512 of them 110 -> 87).
 template <bool kBf16, int kD, int kWaves, bool kSplit>
@@ -479,7 +479,7 @@ struct Geometry {
   static constexpr bool kLarge = kStageBytes > 8 * 1024;
   static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? (kLarge ? 4 : 8) : kLarge && !kSplit ? 2 : 4;
   static constexpr int kGroups = kWaves == 8 ? 1 : kWaves == 4 ? 2 : kLarge && kSplit ? 2 : 4;         // workgroups that a compute unit holds
-  static constexpr int kMostWays = kWaves == 8 || kStages < 4 ? 1 : 2;
+  static constexpr int kMostWays = kWaves == 8 || kStages < 4 ? 1 : 2;       // steps that waves of the same rows may have side by side
   static constexpr int kStateBytes = R::kQuads * 1024 + 512;   // what a wave hands over
   static constexpr int kWavesPerSimd = (kGroups * kWaves + 3) / 4;
   static constexpr int kPlacesAt = kStages * kStageBytes, kIdsAt = kPlacesAt + 2 * kWindow * 8;       // places of K and V, page ids
