@@ -406,7 +406,15 @@ basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, con
  *   keep         [n_seq, most] int32, rows keep_stride >= most entries apart; the first count[i] of a row ascend strictly from 0 or more on.  (Of other lists it is
  *                not defined which rows are moved; an entry below its own place, a place without a page or beyond the table row moves nothing.)
  * The pages that are written to must belong to their sequence alone.  What stood behind the kept tokens stays there.  n_seq * heads * bytes of a row < 2^29.
+ * basa_cache_compact_held: the same within what a sequence holds.
+ *   lens         nullable, [n_seq] int32: tokens that it holds (of a tree: lens of the step, the drafted ones included); kept tokens from there on move
+ *                nothing, and no page behind them is written to.  Without lens a sequence holds what its row has room for: entries behind its tokens, which
+ *                may name pages that others have by now, are then taken for its pages.  A sequence that basa_page_tables did not serve has nothing to keep: its
+ *                lens are `have`, so that of a call with lens and start = have none of its tokens moves; its new length is at most lens.
  */
+basa_status basa_cache_compact_held(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
+                                    const int32_t* lens, const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count,
+                                    int32_t n_seq, void* stream);
 basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
                                const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,
                                void* stream);

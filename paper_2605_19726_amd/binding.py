@@ -30,7 +30,7 @@ EXPORTS = (
     "basa_block_radius", "basa_deviation_bound", "basa_selection_fidelity", "basa_pearson_sums",
     "basa_attn_best_workspace_size", "basa_varlen_workspace_size", "basa_varlen_attn", "basa_static_scratch_size", "basa_static_init", "basa_norm_sort_static",
     "basa_page_tables", "basa_cache_append", "basa_cache_gather", "basa_decode_workspace_size", "basa_decode_attn",
-    "basa_tree_masks", "basa_tree_workspace_size", "basa_tree_attn", "basa_cache_compact", "basa_page_fork", "basa_cache_copy",
+    "basa_tree_masks", "basa_tree_workspace_size", "basa_tree_attn", "basa_cache_compact", "basa_cache_compact_held", "basa_page_fork", "basa_cache_copy",
     "basa_page_free_workspace_size", "basa_page_free",
 )
 
@@ -144,6 +144,8 @@ def load():
     lib.basa_tree_attn.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, V, C.c_int32, C.c_int64, V, S3, V, V, C.c_size_t, V]
     lib.basa_cache_compact.restype = C.c_int
     lib.basa_cache_compact.argtypes = [T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, C.c_int64, V, C.c_int32, V]
+    lib.basa_cache_compact_held.restype = C.c_int
+    lib.basa_cache_compact_held.argtypes = [T, T, V, C.c_int32, C.c_int64, V, V, V, C.c_int32, C.c_int64, V, C.c_int32, V]
     lib.basa_page_fork.restype = C.c_int
     lib.basa_page_fork.argtypes = [V, C.c_int32, C.c_int64, V, C.c_int32, C.c_int32, V, C.c_int32, V, C.c_int32, V, C.c_int64, V, V, V, V]
     lib.basa_cache_copy.restype = C.c_int
@@ -733,13 +735,15 @@ def ba_att_tree(q, k, v, cache: PagedCache, table, lens, slots, cu_seqlens, mask
     return basa_tree_attn(q, cache, table, lens, cu_seqlens, masks, want_lse, ws, out)
 
 
-def basa_cache_compact(cache: PagedCache, table, start, keep, count):
-    """Kept tokens of every sequence moved together, in place: token start[i] + keep[i, j] to start[i] + j, for j < count[i].  keep [n_seq, most]: ascending rows."""
+def basa_cache_compact(cache: PagedCache, table, start, keep, count, lens=None):
+    """Kept tokens of every sequence moved together, in place: token start[i] + keep[i, j] to start[i] + j, for j < count[i].  keep [n_seq, most]: ascending rows.
+    lens [n_seq]: tokens that a sequence holds (PageTables.lens, the drafted ones included): none from there on moves, and no page behind them is written to.  Without it
+    all entries of a table row count as the sequence's pages, also ones that others have by now: of a sequence that was not served, or that was cut back."""
     dev, n = cache.device, start.shape[0]
     tab, width, stride = _block_table(table, n, dev)
     rows, most, keep_stride = _int_rows(keep, "keep", dev, n)
-    _launch(load().basa_cache_compact, dev, cache._kd, cache._vd, tab, width, stride, _int_array(start, "start", dev, (n,)), rows, most, keep_stride,
-            _int_array(count, "count", dev, (n,)), n)
+    _launch(load().basa_cache_compact_held, dev, cache._kd, cache._vd, tab, width, stride, None if lens is None else _int_array(lens, "lens", dev, (n,)),
+            _int_array(start, "start", dev, (n,)), rows, most, keep_stride, _int_array(count, "count", dev, (n,)), n)
 
 
 class PageFork:

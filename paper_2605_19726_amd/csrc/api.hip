@@ -917,9 +917,9 @@ basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, con
                           mask_stride, out, out_t, out_h, lse, ws, reinterpret_cast<hipStream_t>(stream));
 }
 
-basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
-                               const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,
-                               void* stream) {
+basa_status basa_cache_compact_held(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
+                                    const int32_t* lens, const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count,
+                                    int32_t n_seq, void* stream) {
   basa_status s;
   if ((s = check_pages(k_pages, v_pages)) != BASA_OK) return s;
   if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
@@ -928,8 +928,13 @@ basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_
   if (!compact_takes(n_seq, view_of(*k_pages))) {
     set_error("%d sequences of %d heads: more than a call takes", n_seq, k_pages->heads); return BASA_ERR_UNSUPPORTED;
   }
-  return launch_cache_compact(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, start, keep, most, keep_stride, count, n_seq,
+  return launch_cache_compact(view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, start, keep, most, keep_stride, count, n_seq,
                               reinterpret_cast<hipStream_t>(stream));
+}
+basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,
+                               const int32_t* start, const int32_t* keep, int32_t most, int64_t keep_stride, const int32_t* count, int32_t n_seq,
+                               void* stream) {
+  return basa_cache_compact_held(k_pages, v_pages, table, width, table_stride, nullptr, start, keep, most, keep_stride, count, n_seq, stream);
 }
 
 basa_status basa_page_fork(const int32_t* table, int32_t width, int64_t table_stride, const int32_t* lens, int32_t n_seq, int32_t page,

@@ -203,8 +203,8 @@ basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, 
                               int32_t* depths, hipStream_t st);
 bool compact_takes(int n, const TensorView& k_pages);
 basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
-                                 const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
-                                 hipStream_t st);
+                                 const int32_t* lens, const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count,
+                                 int n, hipStream_t st);
 bool page_fork_takes(int n_old, int n_new);
 basa_status launch_page_fork(const int32_t* table, int width, int64_t table_stride, const int32_t* lens, int n_old, int page,
                              const int32_t* parents, int n_new, const int32_t* free_pages, int n_free, int32_t* new_table, int64_t new_stride,

@@ -69,19 +69,23 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* parents,
 struct CompactArgs {
   char *k, *v;
   int64_t k_b, k_h, k_l, v_b, v_h, v_l;     // bytes
-  const int32_t *table, *start, *keep, *count;
+  const int32_t *table, *start, *keep, *count, *lens;       // lens: tokens that a sequence holds, or null: as many as its row has room for
   int64_t table_stride, keep_stride;
   int width, most, pages, row_bits, parts;  // bytes of a row of one head; parts of K and V of a token: of a lane or a workgroup
   FastDiv page;
 };
+// Tokens of a sequence that may be read.  (Entries of its row behind them may be the ids of pages that others have by now.)
+__device__ __forceinline__ int tokens_held(const CompactArgs& a, int seq) {
+  const int room = a.width * (int)a.page.d;      // at most 2^30
+  return a.lens ? min(a.lens[seq], room) : room;
+}
 // Where move j of a sequence reads and writes in K or V, from the head's row on; -1: no move.
 struct Move { int64_t from, to; };
-__device__ __forceinline__ Move move_of(const CompactArgs& a, int seq, int start, int j, int64_t page_bytes, int64_t row_bytes) {
-  const int64_t room = (int64_t)a.width * a.page.d;
+__device__ __forceinline__ Move move_of(const CompactArgs& a, int seq, int held, int start, int j, int64_t page_bytes, int64_t row_bytes) {
   const int kept = a.keep[(int64_t)seq * a.keep_stride + j];
   const int32_t* const row = a.table + (int64_t)seq * a.table_stride;
   const int64_t from = (int64_t)start + kept, to = (int64_t)start + j;
-  if (start < 0 || kept <= j || from >= room) return {-1, -1};
+  if (start < 0 || kept <= j || from >= held) return {-1, -1};
   const int from_page = (int)a.page.div((uint32_t)from), to_page = (int)a.page.div((uint32_t)to);
   const int from_id = row[from_page], to_id = row[to_page];
   if ((unsigned)from_id >= (unsigned)a.pages || (unsigned)to_id >= (unsigned)a.pages) return {-1, -1};
@@ -93,7 +97,7 @@ constexpr int kMoves = 256, kAtOnce = 8;
 __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
   __shared__ Move moves[2][kMoves];         // K, V
   const int seq = blockIdx.x, tid = threadIdx.x, part = blockIdx.y * 256 + tid;
-  const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq];
+  const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq], held = tokens_held(a, seq);
   const bool is_v = part >= a.parts;
   const int c = is_v ? part - a.parts : part;
   const int64_t h = c >> (a.row_bits - 4), in_row = (c & ((1 << (a.row_bits - 4)) - 1)) * 16;
@@ -102,8 +106,8 @@ __global__ __launch_bounds__(256) void compact_kernel(CompactArgs a) {
   for (int j0 = 0; j0 < count; j0 += kMoves) {
     const int n = min(count - j0, kMoves);
     if (tid < n) {
-      moves[0][tid] = move_of(a, seq, start, j0 + tid, a.k_b, a.k_l);
-      moves[1][tid] = move_of(a, seq, start, j0 + tid, a.v_b, a.v_l);
+      moves[0][tid] = move_of(a, seq, held, start, j0 + tid, a.k_b, a.k_l);
+      moves[1][tid] = move_of(a, seq, held, start, j0 + tid, a.v_b, a.v_l);
     }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     __syncthreads();
@@ -128,13 +132,13 @@ template <int kThreads>
 __global__ __launch_bounds__(kThreads, 4) void compact_lines_kernel(CompactArgs a) {
   __shared__ Move moves[3][kThreads];         // of the rows that are written, of those that are read, of the next
   const int seq = blockIdx.x / (2 * a.parts), part = blockIdx.x - seq * 2 * a.parts, tid = threadIdx.x;
-  const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq];
+  const int count = min(max(a.count[seq], 0), a.most), start = a.start[seq], held = tokens_held(a, seq);
   if (count == 0) return;
   const bool is_v = part >= a.parts;
   const int c = is_v ? part - a.parts : part;
   const int64_t h = c >> (a.row_bits - 7), in_row = (c & ((1 << (a.row_bits - 7)) - 1)) * kLine + (tid & 7) * 16;
   char* const rows = (is_v ? a.v + h * a.v_h : a.k + h * a.k_h) + in_row;
-  const int64_t page_bytes = is_v ? a.v_b : a.k_b, row_bytes = is_v ? a.v_l : a.k_l, room = (int64_t)a.width * a.page.d;
+  const int64_t page_bytes = is_v ? a.v_b : a.k_b, row_bytes = is_v ? a.v_l : a.k_l;
   const int32_t* const keep = a.keep + (int64_t)seq * a.keep_stride;
   const int32_t* const table = a.table + (int64_t)seq * a.table_stride;
   // A thread's move of the turn that begins with j0, in three steps: the kept token, the ids of its pages, its place.  (No branches, so that nothing waits within one.)
@@ -148,7 +152,7 @@ __global__ __launch_bounds__(kThreads, 4) void compact_lines_kernel(CompactArgs 
     Pages p;
     p.from = (int64_t)start + k.token;
     p.to = (int64_t)start + k.j;
-    p.valid = k.j < count && start >= 0 && k.token > k.j && p.from < room;
+    p.valid = k.j < count && start >= 0 && k.token > k.j && p.from < held;
     p.from_page = (int)a.page.div(p.valid ? (uint32_t)p.from : 0u);
     p.to_page = (int)a.page.div(p.valid ? (uint32_t)p.to : 0u);
     p.from_id = table[p.from_page];
@@ -488,15 +492,15 @@ bool compact_takes(int n, const TensorView& k) {
   return n <= 1 << 22 && (int64_t)n * k.heads * (k.d * (k.dtype == BASA_BF16 ? 2 : 4) / kLine) * 2 < (1 << 23);
 }
 basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width, int64_t table_stride,
-                                 const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count, int n,
-                                 hipStream_t st) {
+                                 const int32_t* lens, const int32_t* start, const int32_t* keep, int most, int64_t keep_stride, const int32_t* count,
+                                 int n, hipStream_t st) {
   if (n == 0 || most == 0) return BASA_OK;
   CompactArgs a{};
   const int e = k_pages.dtype == BASA_BF16 ? 2 : 4;
   a.k = static_cast<char*>(const_cast<void*>(k_pages.ptr)); a.v = static_cast<char*>(const_cast<void*>(v_pages.ptr));
   a.k_b = k_pages.stride_b * e; a.k_h = k_pages.stride_h * e; a.k_l = k_pages.stride_l * e;
   a.v_b = v_pages.stride_b * e; a.v_h = v_pages.stride_h * e; a.v_l = v_pages.stride_l * e;
-  a.table = table; a.start = start; a.keep = keep; a.count = count; a.table_stride = table_stride; a.keep_stride = keep_stride;
+  a.table = table; a.lens = lens; a.start = start; a.keep = keep; a.count = count; a.table_stride = table_stride; a.keep_stride = keep_stride;
   a.width = width; a.most = most; a.pages = k_pages.batch;
   while ((1 << a.row_bits) < k_pages.d * e) ++a.row_bits;
   a.page = fast_div((uint32_t)k_pages.L);

@@ -114,6 +114,60 @@ def test_kept_tokens_without_a_page_and_lists_that_are_none_stay_in_bounds():
     bd.basa_cache_compact(bd.PagedCache(k, v), table, ints([0, 0]), keep[:, :0], ints([8, 8]))
 
 
+# short lists and long ones; lengths below zero, within the kept tokens, and beyond the row
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("size", [30, 700])
+def test_kept_tokens_within_what_a_sequence_holds(dtype, d, size):
+    rng = np.random.default_rng(size)
+    n, page, pages = 9, 16, 9 * (size + 40) // 16 + 12
+    start = rng.integers(0, 30, n)
+    table = new_tables([size + 40] * n, page, pages, rng)
+    most = size * 2 // 3
+    keep = np.array([np.sort(rng.permutation(size)[:most]) for _ in range(n)], dtype=np.int32)
+    keep[4] = np.arange(1, most + 1)
+    lens = start + rng.integers(0, size, n)
+    lens[0], lens[1], lens[2], lens[3], lens[5] = -7, 0, start[2], 2 ** 31 - 1, start[5] + keep[5][most // 2]
+    k, v = (filled(pages, 2, page, d, dtype, x, i) for i, x in enumerate(("head", "token")))
+    within = np.where(start[:, None] + keep < lens[:, None], keep, -1)                   # an entry that is none moves nothing
+    moves = compact(table, start, within, [most] * n, page, pages)
+    assert len(moves) > most
+    want = [moved(x, moves) for x in (k, v)]
+    bd.basa_cache_compact(bd.PagedCache(k, v), ints(table), ints(start), ints(keep), ints([most] * n), ints(lens))
+    for x, w in zip((k, v), want):
+        assert torch.equal(bits(by_slot(x)), bits(w))
+
+
+@pytest.mark.parametrize("taken", [20, 150])
+def test_a_sequence_that_was_not_served_keeps_nothing_and_writes_into_no_page_of_others(taken):
+    """Two sequences draft; the first is cut back, and its row keeps the ids of the pages behind its length.  They go to the second.  When pages run short
+    the first is not served: none of its drafted tokens may move, least of all within the second's pages."""
+    page, pages, heads, d = 16, 24, 2, 64
+    k, v = (filled(pages, heads, page, d, BF, "head", i) for i in range(2))
+    cache = bd.PagedCache(k, v)
+    table = torch.full((2, 24), -1, dtype=torch.int32, device=DEV)
+    free, count = bd.basa_page_free(table, ints([0, 0]), page, pages)
+    step = bd.basa_page_tables(ints([0, 0]), ints([20 + taken, 10]), table, free[:int(count)], page, tokens=30 + taken)
+    assert step.lens.tolist() == [20 + taken, 10]
+    lens = ints([20, 10])                                            # the first is cut back
+    stale = table[0, 2:-(-(20 + taken) // page)].tolist()
+    free, count = bd.basa_page_free(table, lens, page, pages)
+    need = pages * page - 32                                         # all that there is goes to the second
+    step = bd.basa_page_tables(lens, ints([0, need - 10]), table, free[:int(count)], page, tokens=need)
+    assert step.lens.tolist() == [20, need] and set(stale) & set(table[1].tolist())
+    lens = step.lens
+    free, count = bd.basa_page_free(table, lens, page, pages)
+    assert int(count) == 0
+    step = bd.basa_page_tables(lens, ints([taken, 0]), table, free[:0], page, tokens=taken)
+    assert step.lens.tolist() == [20, need] and step.pages.tolist()[0] == 0 and (step.slots == -1).all()
+    before = [x.clone() for x in (k, v)]
+    keep = torch.arange(1, taken, 2, dtype=torch.int32, device=DEV).expand(2, -1).contiguous()
+    kept = ints([keep.shape[1], 0])
+    bd.basa_cache_compact(cache, table, lens, keep, kept, step.lens)
+    for x, b in zip((k, v), before):
+        assert torch.equal(bits(x), bits(b))
+    assert torch.minimum(lens + kept, step.lens).tolist() == [20, need]
+
+
 # ---------------------------------------------------------------- forks and copies
 def _fork_check(lens, parents, n_free, page, seed, width=None):
     rng = np.random.default_rng(seed)

@@ -67,6 +67,22 @@ def test_cache_compact(lib):  # noqa: F811
     assert call(most=0, keep_stride=0, keep=None) == "BASA_OK"
 
 
+def test_cache_compact_within_lengths(lib):  # noqa: F811
+    def call(k=None, v=None, table=0x1000, n=4, width=10, most=6, start=0x2000, keep=0x3000, count=0x4000, lens=0x5000):
+        k, v = k or pages(), v or pages(ptr=0x4000000)
+        return status_of(lib, lib.basa_cache_compact_held, C.byref(k), C.byref(v), V(table), width, 12, V(lens), V(start), V(keep), most, 6, V(count), n, None)[0]
+    for bad in (dict(v=pages(heads=5)), dict(table=None), dict(width=0), dict(start=None), dict(keep=None), dict(count=None), dict(most=7), dict(n=-1)):
+        assert call(**bad) == INVALID, bad
+    for lens in (0x5000, None):
+        assert call(n=0, table=None, start=None, keep=None, count=None, lens=lens) == "BASA_OK"
+        assert call(most=0, keep=None, lens=lens) == "BASA_OK"
+    z = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    cache = bd.PagedCache(*(torch.zeros(6, 2, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
+    for lens in (z(3), z(2, dtype=torch.int64), z(4)[::2]):
+        with pytest.raises(ValueError, match="lens"):
+            bd.basa_cache_compact(cache, z(2, 4), z(2), z(2, 4), z(2), lens)
+
+
 def test_page_fork(lib):  # noqa: F811
     good = dict(table=0x10000, width=20, stride=20, lens=0x1000, n=10, page=16, parents=0x2000, m=30, free=0x3000, n_free=50, new=0x20000, new_stride=24,
                 new_lens=0x4000, copies=0x5000, pages=0x6000)
