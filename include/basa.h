@@ -391,10 +391,17 @@ basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, i
  *   ws           workspace of basa_tree_workspace_size() bytes.  Nothing in it has to start at zero.
  * Tokens that a query does not see, or whose page is none, carry no weight, whatever their rows hold; a query without any token gets a zero row and lse = -inf, as
  * does one whose scores are all -inf.  Infinite values, accuracy and splitting as with basa_decode_attn; how rows are put together goes by T and n_seq too.
+ * The new tokens are taken to be there: of a sequence that basa_page_tables did not serve, whose lens are `have` while its rows still count in cu_seqlens, the last of
+ * the tokens that it held before would pass for them.  basa_tree_attn_slots does not: of a new token that has no slot it writes a zero row and lse = -inf.
+ *   slots        nullable, [T] int64, as of basa_page_tables.  (Without it: give such a sequence a length of 0, which makes its rows the same.)
  * K and V each reach over less than 2^32 times the largest power of two, up to 256 bytes, that divides their pages' and tokens' strides (BASA_ERR_UNSUPPORTED):
  * 512 GiB and more for stores of whole rows.
  */
 size_t basa_tree_workspace_size(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, int32_t n_seq, int32_t width);
+basa_status basa_tree_attn_slots(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                                 int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
+                                 int32_t words, int64_t mask_stride, const int64_t* slots, void* out, const int64_t* out_strides, float* lse,
+                                 void* ws, size_t ws_bytes, void* stream);
 basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
                            int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
                            int32_t words, int64_t mask_stride, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,

@@ -30,7 +30,7 @@ EXPORTS = (
     "basa_block_radius", "basa_deviation_bound", "basa_selection_fidelity", "basa_pearson_sums",
     "basa_attn_best_workspace_size", "basa_varlen_workspace_size", "basa_varlen_attn", "basa_static_scratch_size", "basa_static_init", "basa_norm_sort_static",
     "basa_page_tables", "basa_cache_append", "basa_cache_gather", "basa_decode_workspace_size", "basa_decode_attn",
-    "basa_tree_masks", "basa_tree_workspace_size", "basa_tree_attn", "basa_cache_compact", "basa_cache_compact_held", "basa_page_fork", "basa_cache_copy",
+    "basa_tree_masks", "basa_tree_workspace_size", "basa_tree_attn", "basa_tree_attn_slots", "basa_cache_compact", "basa_cache_compact_held", "basa_page_fork", "basa_cache_copy",
     "basa_page_free_workspace_size", "basa_page_free",
 )
 
@@ -142,6 +142,8 @@ def load():
     lib.basa_tree_workspace_size.argtypes = [T, T, T, C.c_int32, C.c_int32]
     lib.basa_tree_attn.restype = C.c_int
     lib.basa_tree_attn.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, V, C.c_int32, C.c_int64, V, S3, V, V, C.c_size_t, V]
+    lib.basa_tree_attn_slots.restype = C.c_int
+    lib.basa_tree_attn_slots.argtypes = [T, T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, V, C.c_int32, C.c_int64, V, V, S3, V, V, C.c_size_t, V]
     lib.basa_cache_compact.restype = C.c_int
     lib.basa_cache_compact.argtypes = [T, T, V, C.c_int32, C.c_int64, V, V, C.c_int32, C.c_int64, V, C.c_int32, V]
     lib.basa_cache_compact_held.restype = C.c_int
@@ -700,10 +702,12 @@ def tree_workspace_size(q, cache: PagedCache, table) -> int:
     return int(load().basa_tree_workspace_size(_new_rows_desc(q, "q", cache), cache._kd, cache._vd, table.shape[0], table.shape[1]))
 
 
-def basa_tree_attn(q, cache: PagedCache, table, lens, cu_seqlens, masks=None, want_lse: bool = False, ws=None, out=None):
+def basa_tree_attn(q, cache: PagedCache, table, lens, cu_seqlens, masks=None, want_lse: bool = False, ws=None, out=None, slots=None):
     """Attention of the new tokens of every sequence, packed rows q [T, heads_q, d], sequence i's at cu_seqlens[i] .. cu_seqlens[i + 1] - 1 (a device tensor): each sees
     the first lens[i] tokens of its pages but for the last ones, which are the new tokens themselves (appended before), and of those the ones in its row of `masks`
     [T, words] (basa_tree_masks).  Without masks new token r sees new tokens 0 .. r.  Rows of `out` of no sequence keep what they hold (without `out`: anything).
+    slots [T] (PageTables.slots): the row of a new token without a slot is zero, its lse -inf.  Without it the new tokens of every sequence are taken to be there; a length of 0
+    stands for a sequence that was not served, whose own one still counts the tokens before them alone.
     The launch is sized by the table's width: table[:, :w] with the columns in use is faster than one with room for the longest context there is."""
     lib, dev, n = load(), cache.device, cu_seqlens.shape[0] - 1
     qd = _new_rows_desc(q, "q", cache)
@@ -711,6 +715,7 @@ def basa_tree_attn(q, cache: PagedCache, table, lens, cu_seqlens, masks=None, wa
     tab, width, stride = _block_table(table, n, dev)
     at, cu = _int_array(lens, "lens", dev, (n,)), _int_array(cu_seqlens, "cu_seqlens", dev, (n + 1,))
     seen, words, mask_stride = (None, 0, 0) if masks is None else _int_rows(masks, "masks", dev, T, torch.int64)
+    there = None if slots is None else _int_array(slots, "slots", dev, (T,), torch.int64)
     if out is None:
         out = torch.empty(T, hq, d, dtype=q.dtype, device=dev)
     elif out.shape != q.shape or out.dtype != q.dtype or out.device != dev or out.stride(2) != 1:
@@ -723,16 +728,17 @@ def basa_tree_attn(q, cache: PagedCache, table, lens, cu_seqlens, masks=None, wa
             raise ValueError(f"ws must be a contiguous tensor on {dev}")
         st, sh, _ = out.stride()
         ostr = _TwoStrides(st if T > 1 else 0, sh if hq > 1 else d)
-        _launch(lib.basa_tree_attn, dev, qd, cache._kd, cache._vd, tab, width, stride, at, cu, n, seen, words, mask_stride, out.data_ptr(), ostr,
+        _launch(lib.basa_tree_attn_slots, dev, qd, cache._kd, cache._vd, tab, width, stride, at, cu, n, seen, words, mask_stride, there, out.data_ptr(), ostr,
                 _ptr(lse), ws.data_ptr(), ws.numel())
     return (out, lse) if want_lse else out
 
 
 def ba_att_tree(q, k, v, cache: PagedCache, table, lens, slots, cu_seqlens, masks=None, want_lse: bool = False, ws=None, out=None):
     """One layer of a step with several new tokens per sequence, packed rows q [T, heads_q, d] and k, v [T, heads_kv, d]: they enter the cache at their slots and
-    attend to what their sequence holds.  table, lens, slots, cu_seqlens: of basa_page_tables, masks: of basa_tree_masks, once for all layers."""
+    attend to what their sequence holds.  table, lens, slots, cu_seqlens: of basa_page_tables, masks: of basa_tree_masks, once for all layers.  Rows of a sequence that was
+    not served are zero, their lse -inf."""
     basa_cache_append(k, v, slots, cache)
-    return basa_tree_attn(q, cache, table, lens, cu_seqlens, masks, want_lse, ws, out)
+    return basa_tree_attn(q, cache, table, lens, cu_seqlens, masks, want_lse, ws, out, slots)
 
 
 def basa_cache_compact(cache: PagedCache, table, start, keep, count, lens=None):

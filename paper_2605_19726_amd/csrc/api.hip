@@ -885,10 +885,10 @@ size_t basa_tree_workspace_size(const basa_tensor* q, const basa_tensor* k_pages
   return tree_workspace_bytes(q->L, n_seq, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
 }
 
-basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
-                           int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
-                           int32_t words, int64_t mask_stride, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,
-                           void* stream) {
+basa_status basa_tree_attn_slots(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                                 int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
+                                 int32_t words, int64_t mask_stride, const int64_t* slots, void* out, const int64_t* out_strides, float* lse,
+                                 void* ws, size_t ws_bytes, void* stream) {
   basa_status s;
   if ((s = check_tree(q, k_pages, v_pages, n_seq, width)) != BASA_OK) return s;
   if ((s = check_table(table, n_seq, width, table_stride, k_pages->L)) != BASA_OK) return s;
@@ -896,6 +896,7 @@ basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, con
   if (masks && (words < 1 || mask_stride < words || reinterpret_cast<uintptr_t>(masks) % 8)) {
     set_error("masks: rows of %d words, %lld apart, 8-byte aligned", words, (long long)mask_stride); return BASA_ERR_INVALID_ARG;
   }
+  if (reinterpret_cast<uintptr_t>(slots) % 8) { set_error("slots must be 8-byte aligned"); return BASA_ERR_INVALID_ARG; }
   if (!out) { set_error("null output pointer"); return BASA_ERR_INVALID_ARG; }
   if (reinterpret_cast<uintptr_t>(out) % 16) { set_error("out must be 16-byte aligned"); return BASA_ERR_INVALID_ARG; }
   int64_t out_t = (int64_t)q->heads * q->d, out_h = q->d;
@@ -914,7 +915,14 @@ basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, con
   }
   if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
   return launch_tree_attn(view_of(*q), view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, cu_seqlens, n_seq, masks, words,
-                          mask_stride, out, out_t, out_h, lse, ws, reinterpret_cast<hipStream_t>(stream));
+                          mask_stride, slots, out, out_t, out_h, lse, ws, reinterpret_cast<hipStream_t>(stream));
+}
+basa_status basa_tree_attn(const basa_tensor* q, const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width,
+                           int64_t table_stride, const int32_t* lens, const int32_t* cu_seqlens, int32_t n_seq, const int64_t* masks,
+                           int32_t words, int64_t mask_stride, void* out, const int64_t* out_strides, float* lse, void* ws, size_t ws_bytes,
+                           void* stream) {
+  return basa_tree_attn_slots(q, k_pages, v_pages, table, width, table_stride, lens, cu_seqlens, n_seq, masks, words, mask_stride, nullptr, out,
+                              out_strides, lse, ws, ws_bytes, stream);
 }
 
 basa_status basa_cache_compact_held(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* table, int32_t width, int64_t table_stride,

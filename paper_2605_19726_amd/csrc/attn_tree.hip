@@ -47,6 +47,8 @@ struct TreeArgs {
   int n, tokens, heads_kv, group, pages;    // sequences; rows of q
   int row_tokens;                           // tokens a table row has room for
   FastDiv page, per_token;                  // per_token: division by the group
+  const int64_t* slots;                     // or null: every new token is in its pages
+  int64_t all_slots;
   const uint64_t* masks;                    // or null: chains
   int64_t mask_stride;
   int words;
@@ -776,7 +778,13 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
           }
       }
 
-      const float sum = rw.whole_sum();
+      float sum = rw.whole_sum();
+      // The row of a new token that has no slot is that of a query without any token: of a sequence that was not served the last tokens are none of the new ones.  (Asked for
+      // here: in front of the loop it would take a register in it.)
+      if (a.slots && (uint64_t)a.slots[seq.row0 + my_token] >= (uint64_t)a.all_slots) {
+        rw.m = -INFINITY;
+        sum = 0.f;
+      }
       const int row = row_first + R::column(lane);  // of the unit
       const bool there = row < unit_rows && way == 0;
       const int64_t id = (int64_t)(seq.row0 + my_token) * a.heads_kv * a.group + my_head;
@@ -988,7 +996,7 @@ int tree_place_unit(const TensorView& k, const TensorView& v) {
 
 basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                              int64_t table_stride, const int32_t* lens, const int32_t* cu, int n, const int64_t* masks, int words,
-                             int64_t mask_stride, void* out, int64_t out_st, int64_t out_sh, float* lse, void* ws, hipStream_t st) {
+                             int64_t mask_stride, const int64_t* slots, void* out, int64_t out_st, int64_t out_sh, float* lse, void* ws, hipStream_t st) {
   if (n == 0) return BASA_OK;
   TreeArgs a{};
   const bool bf16 = q.dtype == BASA_BF16;
@@ -1004,6 +1012,7 @@ basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, con
   a.row_tokens = width * k_pages.L;
   a.page = fast_div((uint32_t)k_pages.L);
   a.per_token = fast_div((uint32_t)a.group);
+  a.slots = slots; a.all_slots = (int64_t)k_pages.batch * k_pages.L;
   a.masks = reinterpret_cast<const uint64_t*>(masks); a.words = words; a.mask_stride = mask_stride;
   a.out = static_cast<char*>(out); a.out_t = out_st * e; a.out_h = out_sh * e; a.lse = lse;
   const Variant v = variant_of(a.tokens, n, a.group, q.d, bf16, a.row_tokens);

@@ -197,7 +197,7 @@ int tree_place_unit(const TensorView& k, const TensorView& v);
 size_t tree_workspace_bytes(int tokens, int n, int heads_q, int heads_kv, int d, bool bf16, int row_tokens);
 basa_status launch_tree_attn(const TensorView& q, const TensorView& k_pages, const TensorView& v_pages, const int32_t* table, int width,
                              int64_t table_stride, const int32_t* lens, const int32_t* cu, int n, const int64_t* masks, int words,
-                             int64_t mask_stride, void* out, int64_t out_st, int64_t out_sh, float* lse, void* ws, hipStream_t st);
+                             int64_t mask_stride, const int64_t* slots, void* out, int64_t out_st, int64_t out_sh, float* lse, void* ws, hipStream_t st);
 constexpr int kMaxMaskWords = 64;
 basa_status launch_tree_masks(const int32_t* parents, const int32_t* cu, int n, int tokens, int64_t* masks, int words, int64_t mask_stride,
                               int32_t* depths, hipStream_t st);

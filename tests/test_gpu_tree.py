@@ -308,6 +308,63 @@ def test_lengths_that_do_not_cover_the_new_tokens():
         c.check(*c.run())
 
 
+# in one launch and cut, of few rows and of many
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("room,new", [(128, [5, 3, 9, 0, 2]), (4096, [5, 3, 9, 0, 2]), (4096, [40, 70, 8, 1, 90])])
+def test_rows_of_sequences_that_were_not_served_are_zero(dtype, d, room, new):
+    """Pages run short in the middle of a step: the sequences that were not served keep what they held, and their drafted tokens are in no page."""
+    rng = np.random.default_rng(room + new[0])
+    page, hq, hk, n, spare = 16, 8, 2, len(new), 3
+    have = rng.integers(room // 8, room // 2, n)
+    have[1] = have[1] // page * page                                 # this one and the third need more pages than there are
+    have[2] = have[2] // page * page - 1
+    pages = int(sum(-(-x // page) for x in have)) + 40
+    table = new_tables(have, page, pages, rng, room // page)
+    free = np.setdiff1d(np.arange(pages), table.reshape(-1))
+    k, v = (store(pages, hk, page, d, dtype, "head", DEV, 0.0) for _ in range(2))
+    for x in (k, v):
+        x.copy_(randn(x.shape, 5 + (x is v), dtype))
+    T = sum(new) + spare
+    after = [-(-(h + a) // page) - -(-h // page) for h, a in zip(have, new)]
+    dev_table = ints(table)
+    step = bd.basa_page_tables(ints(have), ints(new), dev_table, ints(free[:after[0]]), page, tokens=T)
+    cu, lens = step.cu.tolist(), step.lens.tolist()
+    served = [x == h + a for x, h, a in zip(lens, have, new)]
+    assert served[0] and not served[1] and not served[2]
+    parents = [random_parents(x, rng) for x in new]
+    seen = [ancestors(x) for x in parents]
+    masks, _ = bd.basa_tree_masks(ints(np.concatenate(parents + [np.zeros(spare)])), step.cu, 2)
+    q, kn, vn = (randn((T, h, d), 9 + i, dtype) for i, h in enumerate((hq, hk, hk)))
+    cache = bd.PagedCache(k, v)
+    for m, s in ((masks, seen), (None, [None] * n)):
+        out, lse = bd.ba_att_tree(q, kn, vn, cache, dev_table, step.lens, step.slots, step.cu, m, want_lse=True)
+        of_zero = torch.where(step.lens == ints(have) + ints(new), step.lens, 0)
+        out0, lse0 = bd.basa_tree_attn(q, cache, dev_table, of_zero, step.cu, m, want_lse=True)
+        for i in range(n):
+            rows = slice(cu[i], cu[i + 1])
+            if not served[i]:
+                assert not out[rows].any() and (lse[rows] == -INF).all() and not out0[rows].any() and (lse0[rows] == -INF).all()
+            else:
+                check_tree(out, lse, q, k, v, dev_table.cpu().numpy(), lens, cu, s, f"{dtype} {d} {room}", only=(i, list(range(new[i]))))
+                check_tree(out0, lse0, q, k, v, dev_table.cpu().numpy(), lens, cu, s, f"{dtype} {d} {room}", only=(i, list(range(new[i]))))
+
+
+def test_slots_that_are_none():
+    """Negative, and beyond the cache; the others' rows are what they are without slots."""
+    for dtype, lens, new in ((BF, [100, 30], [20, 7]), (F32, [3000, 70], [20, 70])):
+        c = Case(dtype, 128, 8, 2, 16, lens, new, 6)
+        out, lse = c.run()
+        all_slots = c.k.shape[0] * 16
+        slots = torch.arange(c.T, dtype=torch.int64, device=DEV) % all_slots
+        none = [int(c.cu[0]) + 3, int(c.cu[0]) + 11, int(c.cu[1]), int(c.cu[1]) + 6]
+        for t, x in zip(none, (-1, all_slots, 2 ** 62, -2 ** 63)):
+            slots[t] = x
+        got, got_lse = c.run(slots=slots)
+        assert not got[none].any() and (got_lse[none] == -INF).all()
+        rest = [t for t in range(int(c.cu[0]), int(c.cu[-1])) if t not in none]
+        assert torch.equal(bits(got[rest]), bits(out[rest])) and torch.equal(got_lse[rest], lse[rest])
+
+
 def test_offsets_that_do_not_ascend_stay_in_bounds():
     c = Case(BF, 64, 4, 2, 16, [60, 40, 300], [8, 8, 8], 5)
     for cu in ([0, 20, 4, 24], [50, 20, 90, 7], [-5, 10, 30, 12], [0, 2 ** 31 - 1, 2 ** 31 - 1, 5], [-2 ** 31, 0, 60, -1]):

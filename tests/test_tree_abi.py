@@ -52,6 +52,22 @@ def test_tree_attn(lib):  # noqa: F811
     assert size() > 0 and size(n=-1) == 0 and size(width=0) == 0 and size(q=tensor(heads=7)) == 0
 
 
+def test_tree_attn_of_slots(lib):  # noqa: F811
+    def call(slots, q=tensor(heads=8, L=40), out=0x5000, ws_bytes=2 ** 40, n=4, lens=0x2000):
+        k, v = pages(), pages(ptr=0x4000000)
+        return status_of(lib, lib.basa_tree_attn_slots, C.byref(q), C.byref(k), C.byref(v), V(0x1000), 10, 12, V(lens), V(0x3000), n, V(0x4000), 1, 1, V(slots),
+                         V(out), None, None, V(0x100000), ws_bytes, None)[0]
+    assert call(0x6004) == INVALID and b"slots" in lib.basa_last_error()
+    for slots in (None, 0x6000):
+        assert call(slots, q=tensor(heads=6)) == INVALID and call(slots, out=None) == INVALID and call(slots, lens=None) == INVALID
+        assert call(slots, ws_bytes=0) == WORKSPACE and call(slots, n=0, lens=None) == "BASA_OK"
+    z = lambda *shape, dtype=torch.int32: torch.zeros(*shape, dtype=dtype)  # noqa: E731
+    cache = bd.PagedCache(*(torch.zeros(6, 2, 16, 64, dtype=torch.bfloat16) for _ in range(2)))
+    for slots in (z(5), z(4, dtype=torch.int64), z(10, dtype=torch.int64)[::2]):
+        with pytest.raises(ValueError, match="slots"):
+            bd.basa_tree_attn(torch.zeros(5, 4, 64, dtype=torch.bfloat16), cache, z(2, 4), z(2), z(3), slots=slots)
+
+
 def test_cache_compact(lib):  # noqa: F811
     good = dict(k=pages(), v=pages(ptr=0x4000000), table=0x1000, width=10, stride=12, start=0x2000, keep=0x3000, most=6, keep_stride=6, count=0x4000, n=4)
 
