@@ -430,6 +430,7 @@ basa_status basa_cache_compact(const basa_tensor* k_pages, const basa_tensor* v_
  * pages; its page that is not full, if there is one, goes to the first of them, and each further one gets a page of its own, in order of j from the start of
  * free_pages, and an entry in `copies`.  An old sequence that is no one's parent ends there (basa_page_free finds its pages).  A new
  * sequence whose parent is none (outside [0, n_seq)) is empty, and so is one that is not served because free pages ran short.
+ * Of an old sequence's page that is not full it is taken that no other old sequence holds it.  That is so of all that grew; of one that was cut back, see basa_page_free.
  *   table, lens  of the n_seq <= 8192 old sequences.  parents [n_new] int32, n_new <= 8192.
  *   free_pages   [n_free] int32: pages that belong to no one, each once.
  *   new_table    out, [n_new, width], rows new_stride apart: entries of pages in use are written, the others left as they were.
@@ -448,8 +449,11 @@ basa_status basa_page_fork(const int32_t* table, int32_t width, int64_t table_st
 basa_status basa_cache_copy(const basa_tensor* k_pages, const basa_tensor* v_pages, const int32_t* copies, int32_t n, void* stream);
 /*
  * The pages that no sequence holds: those of 0 .. n_pages - 1 that are not among the first ceil(lens[i] / page) entries of any row, ascending.  A page that several hold is
- * free when the last of them ends; a sequence that ends, or is cut back, gets its new length and nothing else.  (Whatever else has to be
- * kept has a row: a prefix that stays for later prompts, say.)
+ * free when the last of them ends; a sequence that ends, or is cut back to a multiple of the page or into a page that it alone holds, gets its new length and nothing
+ * else.  (Whatever else has to be kept has a row: a prefix that stays for later prompts, say.)
+ * One that is cut back into a page that others hold too, a whole one that a fork shares, must not be given tokens as it is: they would go into the others' page.  It
+ * goes on through basa_page_fork, with its new length, named twice among the parents: the first of the two keeps the shared page and is dropped (a length of 0), the second
+ * has a copy.
  *   n_seq up to 2^22, n_pages up to 2^26.
  *   free_pages   out [n_pages] int32: the free ones come first, the rest is left as it was.   count: out [1] int32, how many.
  *   ws           workspace of basa_page_free_workspace_size() bytes.  Nothing in it has to start at zero.

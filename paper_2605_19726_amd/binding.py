@@ -769,7 +769,8 @@ class PageFork:
 
 def basa_page_fork(table, lens, parents, free_pages, page: int, out: Optional[PageFork] = None) -> PageFork:
     """Block tables of sequences that go on from others: new sequence j is old sequence parents[j].  Whole pages are shared; the copies of pages that are not full
-    are made by basa_cache_copy."""
+    are made by basa_cache_copy.  A sequence that was cut back into a page that others hold too is named twice: the first of the two keeps that page and is dropped, the
+    second has a copy."""
     dev, n, m = table.device, lens.shape[0], parents.shape[0]
     tab, width, stride = _block_table(table, n, dev)
     if out is None:

@@ -388,6 +388,58 @@ def test_a_serving_loop_with_drafted_trees_samples_and_freed_pages(dtype, d):
     assert int(count) == pages
 
 
+@pytest.mark.parametrize("back", [[100, 40], [33, 40], [100, 48], [48, 0], [40, 100, 40]])
+def test_sequences_that_are_cut_back_into_pages_of_a_fork_go_on_with_copies(back):
+    """Samples of one prompt share its whole pages; cut back to `back` tokens, some of them within those, they get new tokens.  Everyone's tokens are their own."""
+    dtype, d, hq, hk, page, pages, prompt, n = BF, 64, 4, 2, 16, 60, 100, len(back)
+    k_cache, v_cache = (store(pages, hk, page, d, dtype, "head", DEV) for _ in range(2))
+    cache = bd.PagedCache(k_cache, v_cache)
+    seed = [0]
+
+    def rows(T):
+        seed[0] += 3
+        return (randn((T, h, d), seed[0] + i, dtype) for i, h in enumerate((hq, hk, hk)))
+
+    def grow(table, lens, add, held):
+        free, count = bd.basa_page_free(table, lens, page, pages)
+        step = bd.basa_page_tables(lens, ints(add), table, free[:int(count)], page, tokens=sum(add))
+        given, asked = step.pages.tolist()
+        assert given == asked
+        q, k, v = rows(sum(add))
+        out, lse = bd.ba_att_tree(q, k, v, cache, table, step.lens, step.slots, step.cu, want_lse=True)
+        cu = step.cu.tolist()
+        held = [tuple(torch.cat([x, y[cu[i]:cu[i + 1]]]) for x, y in zip(held[i], (k, v))) for i in range(len(held))]
+        own = [torch.zeros(len(held), hk, 512, d, dtype=dtype, device=DEV) for _ in range(2)]
+        for i, kv in enumerate(held):
+            for c, x in zip(own, kv):
+                c[i, :, :x.shape[0]] = x.transpose(0, 1)
+        check_tree(out, lse, q, *own, np.arange(len(held))[:, None], step.lens.tolist(), cu, [None] * len(held))
+        return step.lens, held
+
+    none = torch.empty(0, hk, d, dtype=dtype, device=DEV)
+    table = torch.full((1, 20), -1, dtype=torch.int32, device=DEV)
+    lens, held = grow(table, ints([0]), [prompt], [(none, none)])
+
+    def fork(table, lens, parents, held):
+        free, count = bd.basa_page_free(table, lens, page, pages)
+        f = bd.basa_page_fork(table, lens, ints(parents), free[:int(count)], page)
+        bd.basa_cache_copy(cache, f.copies)
+        given, asked = f.pages.tolist()
+        assert given == asked
+        return f.table, f.lens, [held[p] for p in parents]
+    table, lens, held = fork(table, lens, [0] * n, held)
+    lens, held = grow(table, lens, [5 + i for i in range(n)], held)
+    lens, held = ints(back), [tuple(x[:b] for x in kv) for b, kv in zip(back, held)]
+    # within the whole pages of the prompt and not at the end of one: named twice, the first of the two is dropped
+    parents = [i for i, b in enumerate(back) for _ in range(1 + (b < prompt // page * page and b % page > 0))]
+    table, lens, held = fork(table, lens, parents, held)
+    left = [j for j, p in enumerate(parents) if p not in parents[j + 1:]]
+    table, lens, held = table[left].contiguous(), lens[left].contiguous(), [held[j] for j in left]
+    for add in ([1] * n, [3, 30, 17][:n], [20] * n):
+        lens, held = grow(table, lens, add, held)
+    assert lens.tolist() == [len(x[0]) for x in held]
+
+
 def test_a_captured_step_of_all_operators():
     hq, hk, d, page, pages, width, n = 8, 2, 64, 16, 200, 20, 3
     k_cache, v_cache = (filled(pages, hk, page, d, BF, "head", i) for i in range(2))
