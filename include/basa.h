@@ -385,10 +385,10 @@ basa_status basa_tree_masks(const int32_t* parents, const int32_t* cu_seqlens, i
  *   masks        nullable, [T, words] int64, as of basa_tree_masks; any bits do, a token need not see itself.  New tokens without a bit (from 64 *
  *                words on) are seen by no one.  NULL: chains, new token r sees new tokens 0 .. r.
  *   out          [T, heads_q, d], dtype of q, 16-byte aligned; rows of no sequence are left as they were.  out_strides: nullable HOST array of 2,
- *                strides of its token and head axes in elements (multiples of 16 bytes, head stride >= d).  Rows of out must not alias each other or an
- *                input.
+ *                strides of its token and head axes in elements (multiples of 16 bytes, head stride >= d).  Rows of out must not alias each other.
  *   lse          out, nullable, [T, heads_q] float.
  *   ws           workspace of basa_tree_workspace_size() bytes.  Nothing in it has to start at zero.
+ * out, lse and ws must not overlap an input or each other (BASA_ERR_INVALID_ARG); rows of out may lie between those of q.
  * Tokens that a query does not see, or whose page is none, carry no weight, whatever their rows hold; a query without any token gets a zero row and lse = -inf, as
  * does one whose scores are all -inf.  Infinite values, accuracy and splitting as with basa_decode_attn; how rows are put together goes by T and n_seq too.
  * The new tokens are taken to be there: of a sequence that basa_page_tables did not serve, whose lens are `have` while its rows still count in cu_seqlens, the last of

@@ -8,6 +8,7 @@
 #include <mutex>
 #include <vector>
 #include "common.hpp"
+#include "row_sets.hpp"
 
 namespace basa {
 
@@ -450,6 +451,24 @@ basa_status check_apart(const Span* in, size_t n_in, const Span* out, size_t n_o
   return BASA_OK;
 }
 size_t rows_span(int32_t n, int64_t stride, int32_t width, size_t e) { return n > 0 ? ((size_t)(n - 1) * stride + width) * e : 0; }
+// The same of tensors by their rows: one may stand between the rows of another.
+struct Rows { RowSet set; const char* name; };
+basa_status check_apart(const Rows* in, size_t n_in, const Rows* out, size_t n_out) {
+  for (size_t o = 0; o < n_out; ++o) {
+    for (size_t i = 0; i < n_in; ++i)
+      if (overlap(out[o].set, in[i].set)) { set_error("%s must not overlap %s", out[o].name, in[i].name); return BASA_ERR_INVALID_ARG; }
+    for (size_t p = 0; p < o; ++p)
+      if (overlap(out[o].set, out[p].set)) { set_error("%s must not overlap %s", out[o].name, out[p].name); return BASA_ERR_INVALID_ARG; }
+  }
+  return BASA_OK;
+}
+RowSet rows_of(const basa_tensor& t) {
+  const uint64_t e = t.dtype == BASA_BF16 ? 2 : 4;
+  return row_set(t.ptr, t.d * e, {(uint64_t)t.batch, (uint64_t)t.heads, (uint64_t)t.L}, {t.stride_b * e, t.stride_h * e, t.stride_l * e});
+}
+RowSet rows_of(const void* at, int64_t n, int64_t stride, int64_t width, uint64_t e) {
+  return row_set(at, width * e, {(uint64_t)n, 1, 1}, {stride * e, 0, 0});
+}
 
 }  // namespace
 }  // namespace basa
@@ -907,6 +926,7 @@ basa_status basa_tree_attn_slots(const basa_tensor* q, const basa_tensor* k_page
       set_error("out_strides must be non-negative multiples of 16 bytes with the head stride >= d");
       return BASA_ERR_INVALID_ARG;
     }
+    if (q->L > 1 && out_t < q->d) { set_error("rows of out must not alias each other"); return BASA_ERR_INVALID_ARG; }
   }
   const size_t need = tree_workspace_bytes(q->L, n_seq, q->heads, k_pages->heads, q->d, q->dtype == BASA_BF16, width * k_pages->L);
   if (!ws || ws_bytes < need) {
@@ -914,6 +934,15 @@ basa_status basa_tree_attn_slots(const basa_tensor* q, const basa_tensor* k_page
     return BASA_ERR_WORKSPACE;
   }
   if (reinterpret_cast<uintptr_t>(ws) % 256) { set_error("workspace must be 256-byte aligned"); return BASA_ERR_INVALID_ARG; }
+  if (n_seq == 0) return BASA_OK;
+  // A workgroup reads rows of q when another one has written its own.
+  const uint64_t e = q->dtype == BASA_BF16 ? 2 : 4;
+  const Rows in[] = {{rows_of(*q), "q"}, {rows_of(*k_pages), "k_pages"}, {rows_of(*v_pages), "v_pages"}, {rows_of(table, n_seq, table_stride, width, 4), "table"},
+                     {row_set(lens, (uint64_t)n_seq * 4), "lens"}, {row_set(cu_seqlens, ((uint64_t)n_seq + 1) * 4), "cu_seqlens"},
+                     {rows_of(masks, q->L, mask_stride, words, 8), "masks"}, {row_set(slots, (uint64_t)q->L * 8), "slots"}};
+  const Rows outs[] = {{row_set(out, q->d * e, {(uint64_t)q->L, (uint64_t)q->heads, 1}, {out_t * e, out_h * e, 0}), "out"},
+                       {row_set(lse, (uint64_t)q->L * q->heads * 4), "lse"}, {row_set(ws, need), "the workspace"}};
+  if ((s = check_apart(in, 8, outs, 3)) != BASA_OK) return s;
   return launch_tree_attn(view_of(*q), view_of(*k_pages), view_of(*v_pages), table, width, table_stride, lens, cu_seqlens, n_seq, masks, words,
                           mask_stride, slots, out, out_t, out_h, lse, ws, reinterpret_cast<hipStream_t>(stream));
 }

@@ -185,6 +185,28 @@ def test_rows_of_no_sequence_and_what_lies_between_strided_rows_stay_as_they_wer
         assert (wide[kept] == 5.0).all()
 
 
+def test_outputs_lie_in_no_other_tensor_but_may_lie_between_rows_of_the_queries():
+    for dtype in (BF, F32):
+        c = Case(dtype, 64, 8, 2, 16, [5000, 300, 30], [10, 40, 0], 9)
+        out, lse = c.run()
+        both = torch.full((c.T, 16, 64), 5.0, dtype=dtype, device=DEV)
+        rows = slice(int(c.cu[0]), int(c.cu[-1]))
+        for q, o in ((both[:, :8], both[:, 8:]), (both[:, ::2], both[:, 1::2])):
+            q.copy_(c.q)
+            _, lse2 = bd.basa_tree_attn(q, c.cache(), ints(c.table), ints(c.lens), ints(c.cu), c.masks, want_lse=True, out=o)
+            assert torch.equal(bits(o[rows].contiguous()), bits(out[rows])) and torch.equal(lse2[rows], lse[rows]) and torch.equal(bits(q.contiguous()), bits(c.q))
+        for o in (c.q, c.q.new_empty(1, 8, 64).expand(c.T, 8, 64), c.k.reshape(-1)[:c.q.numel()].view(c.q.shape)):
+            with pytest.raises(RuntimeError, match="overlap|alias"):
+                c.run(out=o)
+        need = bd.tree_workspace_size(c.q, c.cache(), ints(c.table))
+        ws = torch.empty(need + 2 ** 20, dtype=torch.uint8, device=DEV)
+        with pytest.raises(RuntimeError, match="overlap"):
+            c.run(ws=ws, out=ws[need // 256 * 256 - 256:][:c.q.numel() * c.q.element_size()].view(dtype).view(c.q.shape))
+        behind = ws[-(-need // 256) * 256:][:c.q.numel() * c.q.element_size()].view(dtype).view(c.q.shape)
+        c.run(ws=ws, out=behind)
+        assert torch.equal(bits(behind[rows]), bits(out[rows]))
+
+
 def test_masks_of_any_kind():
     """Bits that are no tree's: rows that see nothing at all, not themselves, later ones; bits behind the last new token; fewer words than tokens."""
     for dtype in (BF, F32):

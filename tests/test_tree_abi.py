@@ -68,6 +68,35 @@ def test_tree_attn_of_slots(lib):  # noqa: F811
             bd.basa_tree_attn(torch.zeros(5, 4, 64, dtype=torch.bfloat16), cache, z(2, 4), z(2), z(3), slots=slots)
 
 
+def test_tree_attn_refuses_outputs_in_other_tensors(lib):  # noqa: F811
+    """One tensor is moved into another at a time, at its first and at its last bytes."""
+    q, k, v = tensor(ptr=2 ** 33, heads=8, L=40, stride_l=3 * 1024, stride_h=128), pages(ptr=2 ** 34), pages(ptr=2 ** 35)
+    need = lib.basa_tree_workspace_size(C.byref(q), C.byref(k), C.byref(v), 4, 10)
+    at = dict(table=2 ** 36, lens=2 ** 37, cu=2 ** 38, masks=2 ** 39, slots=2 ** 40, out=2 ** 41, lse=2 ** 42, ws=2 ** 43)
+    size = dict(q=40 * 3 * 2048 - 2 * 2048, k=100 * 16 * 4 * 256, v=100 * 16 * 4 * 256, table=4 * (3 * 12 + 10), lens=16, cu=20, masks=8 * (39 * 3 + 2), slots=320,
+                out=39 * 2560 + 7 * 288 + 256, lse=40 * 8 * 4, ws=need)
+    where = dict(at, q=2 ** 33, k=2 ** 34, v=2 ** 35)
+
+    def call(**kw):
+        a = dict(at, **kw)
+        return status_of(lib, lib.basa_tree_attn_slots, C.byref(q), C.byref(k), C.byref(v), V(a["table"]), 10, 12, V(a["lens"]), V(a["cu"]), 4, V(a["masks"]), 2, 3,
+                         V(a["slots"]), V(a["out"]), (C.c_int64 * 2)(1280, 144), V(a["lse"]), V(a["ws"]), need, None)[0]
+    unit = dict(out=16, lse=4, ws=256)
+    for o in ("out", "lse", "ws"):
+        for other in where:
+            if other == o:
+                continue
+            up = lambda x: -(-x // unit[o]) * unit[o]  # noqa: E731
+            ends = [where[other], (where[other] + size[other] - 1) // unit[o] * unit[o]]          # its first unit and its last
+            ends.append(up(where[other] - size[o] + 1))                                           # its first byte under the last of `o`
+            for x in ends:
+                assert call(**{o: x}) == INVALID, (o, other, x)
+                assert b"overlap" in lib.basa_last_error()
+    twice = (C.c_int64 * 2)(120, 128)
+    assert status_of(lib, lib.basa_tree_attn_slots, C.byref(q), C.byref(k), C.byref(v), V(at["table"]), 10, 12, V(at["lens"]), V(at["cu"]), 4, None, 0, 0, None, V(at["out"]),
+                     twice, None, V(at["ws"]), need, None)[0] == INVALID
+
+
 def test_cache_compact(lib):  # noqa: F811
     good = dict(k=pages(), v=pages(ptr=0x4000000), table=0x1000, width=10, stride=12, start=0x2000, keep=0x3000, most=6, keep_stride=6, count=0x4000, n=4)
 
