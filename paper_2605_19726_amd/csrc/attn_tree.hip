@@ -109,12 +109,13 @@ __device__ __forceinline__ void store4(char* at, floatx4 o) {
 }
 // 16 bytes from memory for every lane, side by side into the LDS.  Written in assembly, without a register for its result: the compiler would wait for all of
 // these before it reads the LDS or meets a barrier; the waits stand where the ring needs them.  As a stream that no cache keeps: 8 new tokens of 32 sequences 130 us, and 148
-// without that; level where a KV head has several tiles and reads its rows as often.
+// without that; level where a KV head has several tiles and reads its rows as often.  m0, the place in the LDS, is an operand, so that the compiler knows when it changes; between
+// its write and such a load there has to be an instruction.
 __device__ __forceinline__ void to_lds(const char* from, uint32_t at) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "s"(at) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(from), "{m0}"(at) : "memory");
 }
 __device__ __forceinline__ void word_to_lds(const void* from, uint32_t at) {      // 4 bytes for every lane
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "s"(at) : "memory");
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(from), "{m0}"(at) : "memory");
 }
 // Everyone's LDS operations are done before anyone goes on.  Requests by to_lds that are under way stay so.
 __device__ __forceinline__ void meet() {

@@ -120,3 +120,28 @@ def test_no_kernel_spills():
             elif m and int(m.group(2)):
                 found[kernel] = int(m.group(2))
     assert kernels > 20 and found == {}
+
+
+def test_m0_is_an_operand_of_the_assembly_that_reads_it():
+    """The compiler may keep a value in m0 across a statement that writes it unsaid: loads into the LDS take it as an operand, and no statement sets it."""
+    found = 0
+    for name in sorted(os.listdir(build.CSRC)):
+        text = open(os.path.join(build.CSRC, name)).read()
+        for m in re.finditer(r"\basm\b(?:\s+volatile)?\s*\((.*?)\);", text, re.S):
+            assert not re.search(r"\bs_\w+\s+m0\b", m.group(1)), f"{name}: {m.group(0)}"
+            if "load_lds" in m.group(1):
+                found += 1
+                assert '"{m0}"' in m.group(1), f"{name}: {m.group(0)}"
+    assert found >= 2
+    # what became of it: every such load has a write of m0 before it in its block, and no other load between the two
+    (path,) = [f for f in _asm_files() if os.path.basename(f).startswith("attn_tree-")]
+    loads, written = 0, False
+    for line in open(path):
+        if re.match(r"\.?\w+:", line):
+            written = False
+        elif re.match(r"\s*s_\w+ m0,", line):
+            written = True
+        elif "global_load_lds" in line:
+            assert written, line
+            loads, written = loads + 1, False
+    assert loads > 100
