@@ -66,8 +66,9 @@ struct TreeArgs {
 constexpr int kPlanBatch = 512;             // up to this many sequences every wave sums up the lengths by itself
 constexpr int kWindow = 256;                // tokens whose places in the cache are in the LDS, twice
 // How far a row's scores, in units of the exponent, may rise above the maximum that its weights refer to before these are scaled: weights up to 2^8 are as exact as
-// weights up to 1.
-constexpr float kRise = 8.f;
+// weights up to 1.  Sums of large values could be no number for it where they are one with weights up to 1: from kLarge on they are made again with those.  (Below it
+// those of all parts of a row, 1024 at most, are a number.)
+constexpr float kRise = 8.f, kLarge = 0x1p117f;
 
 struct Sequence { int len, row0, n; };
 __device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
@@ -197,7 +198,7 @@ struct Rows<true, kD> {
     }
   }
   template <class F>
-  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, int lane, F meanwhile) {
+  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, float rise, int lane, F meanwhile) {
     floatx16 s;
     bf16x8 v[2][kBlocks];
     scores(s, k_lds, lane, [&] {
@@ -213,7 +214,7 @@ struct Rows<true, kD> {
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = fmaxf(pair_max<32>(top) * scale, m);
-    if (__ballot(top > m + kRise)) {
+    if (__ballot(top > m + rise)) {
       const float f = factor_of(m, top);
       m = top;
       l *= f;
@@ -285,13 +286,13 @@ struct Rows<true, kD> {
     }
     return v;
   }
-  __device__ __forceinline__ bool any_nan() const {
+  __device__ __forceinline__ bool any_nan_or_large() const {
     float x = 0.f;
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x = __builtin_elementwise_maximum(x, acc[e][i]);
-    return __ballot(x != x) != 0;
+      for (int i = 0; i < 16; ++i) x = __builtin_elementwise_maximum(x, fabsf(acc[e][i]));
+    return __ballot(!(x < kLarge)) != 0;
   }
   __device__ __forceinline__ float whole_sum() const { return pair_sum<32>(l); }
   static __device__ __forceinline__ bool writes_sum(int lane) { return lane < 32; }
@@ -379,7 +380,7 @@ struct Rows<false, kD> {
     }
   }
   template <class F>
-  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, int lane, F meanwhile) {
+  __device__ __forceinline__ void step(uint32_t k_lds, uint32_t v_lds, float scale, float rise, int lane, F meanwhile) {
     floatx4 s;
     uintx4 v[4][kD / 64];
     scores(s, k_lds, lane, [&] {
@@ -393,7 +394,7 @@ struct Rows<false, kD> {
     });
     float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     top = fmaxf(pair_max<16>(pair_max<32>(top)) * scale, m);
-    if (__ballot(top > m + kRise)) {
+    if (__ballot(top > m + rise)) {
       const float f = factor_of(m, top);
       m = top;
       l *= f;
@@ -444,13 +445,13 @@ struct Rows<false, kD> {
       if ((v[i] & 0x7f800000u) == 0x7f800000u) v[i] = 0u;
     return v;
   }
-  __device__ __forceinline__ bool any_nan() const {
+  __device__ __forceinline__ bool any_nan_or_large() const {
     float x = 0.f;
 #pragma unroll
     for (int e = 0; e < kBlocks; ++e)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x = __builtin_elementwise_maximum(x, acc[e][i]);
-    return __ballot(x != x) != 0;
+      for (int i = 0; i < 4; ++i) x = __builtin_elementwise_maximum(x, fabsf(acc[e][i]));
+    return __ballot(!(x < kLarge)) != 0;
   }
   __device__ __forceinline__ float whole_sum() const { return pair_sum<16>(pair_sum<32>(l)); }
   static __device__ __forceinline__ bool writes_sum(int lane) { return lane < 16; }
@@ -713,8 +714,8 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
         }
         return s;
       };
-      // Once as it is.  A weight of zero, or a part of one that is, times infinity or NaN is NaN, also where a row does not see the token: if there is NaN in the result
-      // of a workgroup, once more with the values that are finite, and then the others added to the rows that see them.
+      // Once as it is.  A weight of zero, or a part of one that is, times infinity or NaN is NaN, also where a row does not see the token: if there is NaN, or a sum that is
+      // too large, in the result of a workgroup, once more with the values that are finite and with weights up to 1, and then the others added to the rows that see them.
       bool clean = false;
 #pragma clang loop unroll(disable)
       for (;;) {
@@ -733,7 +734,7 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
             return;
           }
           const uint32_t stage = stage_of(t + way);
-          rw.step(stage + k_lane, stage + G::kHalfBytes + v_lane, a.scale_log2e, lane, [&] {
+          rw.step(stage + k_lane, stage + G::kHalfBytes + v_lane, a.scale_log2e, clean ? 0.f : kRise, lane, [&] {
             const Seen seen = seen_of(t + way);
             next();
             return seen;
@@ -742,7 +743,7 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
         if (clean) break;
         if (tid == 0) *vote = 0;
         meet();
-        if (works && rw.any_nan() && lane == 0) *vote = 1;
+        if (works && rw.any_nan_or_large() && lane == 0) *vote = 1;
         meet();
         if (!*vote) break;
         clean = true;
@@ -880,8 +881,23 @@ __global__ __launch_bounds__(kJoinThreads) void tree_join_kernel(TreeArgs a, int
     m = top;
     l = l * f + l2 * x;
   }
+  o = normalised(o, l);
+  // Parts that are numbers and a sum that is none: every part by its share of the whole sum.
+  const float most = __builtin_elementwise_maximum(__builtin_elementwise_maximum(fabsf(o[0]), fabsf(o[1])), __builtin_elementwise_maximum(fabsf(o[2]), fabsf(o[3])));
+  if (__ballot(!(most < INFINITY))) {
+    const float by = 1.0f / l;
+    o = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int w = g0 + lane / kLanes; w <= g1; w += kSubs) {
+      const int64_t place = (int64_t)(2 * w + (w == g0)) * tile + row;
+      o += *reinterpret_cast<const floatx4*>(a.part_o + place * kD + 4 * c) * factor_of(a.part_ml[place].x, m) * by;
+    }
+#pragma unroll
+    for (int off = kLanes; off < 64; off *= 2)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += __shfl_xor(o[i], off);
+  }
   if (lane >= kLanes) return;
-  store4<kBf16>(a.out + t * a.out_t + head * a.out_h + c * 4 * kElem, normalised(o, l));
+  store4<kBf16>(a.out + t * a.out_t + head * a.out_h + c * 4 * kElem, o);
   if (a.lse && c == 0) a.lse[id] = lse_of(m, l);
 }
 

@@ -306,6 +306,42 @@ def test_values_that_are_not_finite_of_few_rows(dtype, d, lens):
         c.v.copy_(v)
 
 
+# in one launch and cut; few rows and many; scores that rise by less than 8 in units of the exponent of 2, and by more, from step to step
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
+@pytest.mark.parametrize("n,new,room", [(120, 5, 128), (5000, 5, 5008), (5000, 60, 5008)])
+@pytest.mark.parametrize("rise", [5.4375, 7.5])
+def test_large_values_stay_finite(dtype, d, n, new, room, rise):
+    """Values whose sum over all tokens is a number: of the whole call, and of one KV head with values that are not large beside it."""
+    c = Case(dtype, d, 4, 2, 16, [n, 40], [new, 8], 17, width=room // 16, chain=True)
+    at, off = (x.to(DEV) for x in rows_of(c.table[0], n, 16))
+    c.q[:], c.k[at, :, off] = 0, 0
+    c.q[:, :, 0] = d ** 0.5                                          # scores: what stands in the keys' first place
+    scores = torch.linspace(0, rise, n, device=DEV)
+    scores[torch.arange(n, device=DEV) % 64 >= 32] = rise * 0.99     # large ones in every second 32 tokens
+    scores[:32] = 0
+    c.k[at, :, off, 0] = scores[:, None].to(dtype)
+    size = 3e38 / n
+    c.v[at, 0, off] = (size * (0.5 + 0.5 * torch.rand(n, d, device=DEV, generator=torch.Generator(DEV).manual_seed(5)))).to(dtype)
+    out, lse = c.run()
+    assert torch.isfinite(out[int(c.cu[0]):int(c.cu[-1])].float()).all()
+    c.check(out, lse, f"{dtype} d={d} {n} {rise}")
+
+
+def test_parts_whose_sum_is_no_number_are_averaged():
+    """Every part of a cut sequence has a sum, all of them together have not; with scores of equal size, and with most of the weight in few tokens."""
+    for dtype in (BF, F32):
+        for peak in (0.0, 6.0):
+            c = Case(dtype, 64, 4, 2, 16, [20000], [7], 18, q_scale=0.1, chain=True)
+            at, off = (x.to(DEV) for x in rows_of(c.table[0], 20000, 16))
+            c.v[at, :, off] = (2e35 * (1 + c.v[at, :, off].float().clamp(-1, 1))).to(dtype)
+            c.q[:, :, 0] = 8.0
+            c.k[at, :, off, 0] = 0
+            c.k[at[77::1000], :, off[77::1000], 0] = peak
+            out, lse = c.run()
+            assert torch.isfinite(out[int(c.cu[0]):int(c.cu[-1])].float()).all()
+            c.check(out, lse, f"{dtype} {peak}")
+
+
 def test_scores_that_are_minus_infinity():
     for dtype in (BF, F32):
         c = Case(dtype, 64, 2, 1, 16, [50], [4], 3, around=(0, 0))
