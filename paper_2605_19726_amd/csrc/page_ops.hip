@@ -299,9 +299,10 @@ __global__ __launch_bounds__(256) void cache_copy_kernel(CopyArgs a) {
   const int32_t* const c = a.copies + 3 * (int64_t)blockIdx.x;
   const int from = c[0], to = c[1], tokens = min(max(c[2], 0), a.page);
   if ((unsigned)from >= (unsigned)a.pages || (unsigned)to >= (unsigned)a.pages || from == to) return;
-  const int items = (a.by_token ? tokens : a.page) * a.heads << a.chunk_bits;
-  for (int i = blockIdx.y * 256 + threadIdx.x; i < items; i += gridDim.y * 256) {
-    const int row = i >> a.chunk_bits, outer = (int)a.inner.div(row), in = row - outer * (int)a.inner.d;
+  // (Less than 2^31 of them; a lane's number passes that on its way out.)
+  const uint32_t items = (uint32_t)((a.by_token ? tokens : a.page) * a.heads) << a.chunk_bits;
+  for (uint32_t i = blockIdx.y * 256 + threadIdx.x; i < items; i += gridDim.y * 256) {
+    const int row = (int)(i >> a.chunk_bits), outer = (int)a.inner.div(row), in = row - outer * (int)a.inner.d;
     const int64_t h = a.by_token ? in : outer, t = a.by_token ? outer : in, at = (i & ((1 << a.chunk_bits) - 1)) * 16;
     if (t >= tokens) continue;
     const uintx4 k = *reinterpret_cast<const uintx4*>(a.k + from * a.k_b + h * a.k_h + t * a.k_l + at);

@@ -232,6 +232,20 @@ def test_copies_of_pages(dtype, d, heads, page, layout):
     bd.basa_cache_copy(bd.PagedCache(k, v), ints(np.zeros((0, 3))))
 
 
+def test_copies_of_the_largest_pages():
+    """Pages of nearly 2^31 pieces of 16 bytes, so that a lane's next one lies beyond that.  (Of heads and tokens side by side on the same memory: a page is a strip of it.)"""
+    heads, page, d = 65472, 1025, 128
+    assert 0 < 2 ** 31 - page * heads * 32 < 64 * 256
+    strip = (heads + page) * d
+    k, v = (randn((3 * strip,), 3 + i, F32).as_strided((3, heads, page, d), (strip, d, d, 1)) for i in range(2))
+    before = [torch.as_strided(x, (3 * strip,), (1,)).clone() for x in (k, v)]
+    bd.basa_cache_copy(bd.PagedCache(k, v), ints([[0, 2, 3], [1, 1, page], [3, 0, 5]]))
+    for x, b in zip((k, v), before):
+        want = b.clone()
+        want[2 * strip:2 * strip + (heads + 2) * d] = b[:(heads + 2) * d]
+        assert torch.equal(torch.as_strided(x, (3 * strip,), (1,)), want)
+
+
 # pages, or heads, more than 4 GiB apart in all
 @pytest.mark.parametrize("strides", [(2 ** 28 + 8, 1000, 2 ** 15 + 24), (2 ** 13, 2 ** 31 + 64, 136)])
 def test_moves_and_copies_of_pages_beyond_32_bits(strides):
