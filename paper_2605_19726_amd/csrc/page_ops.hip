@@ -502,7 +502,9 @@ basa_status launch_cache_compact(const TensorView& k_pages, const TensorView& v_
   a.k_b = k_pages.stride_b * e; a.k_h = k_pages.stride_h * e; a.k_l = k_pages.stride_l * e;
   a.v_b = v_pages.stride_b * e; a.v_h = v_pages.stride_h * e; a.v_l = v_pages.stride_l * e;
   a.table = table; a.lens = lens; a.start = start; a.keep = keep; a.count = count; a.table_stride = table_stride; a.keep_stride = keep_stride;
-  a.width = width; a.most = most; a.pages = k_pages.batch;
+  a.width = width; a.pages = k_pages.batch;
+  most = std::min(most, width * k_pages.L);       // entry j moves to j or further on: beyond the row none does (and j stays below 2^30)
+  a.most = most;
   while ((1 << a.row_bits) < k_pages.d * e) ++a.row_bits;
   a.page = fast_div((uint32_t)k_pages.L);
   ProfScope prof(K_PAGED, st);

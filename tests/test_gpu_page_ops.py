@@ -168,6 +168,25 @@ def test_a_sequence_that_was_not_served_keeps_nothing_and_writes_into_no_page_of
     assert torch.minimum(lens + kept, step.lens).tolist() == [20, need]
 
 
+def test_lists_that_are_longer_than_a_row():
+    """As many entries as a call can name, all of them counted: those that a row has room for matter, and no others are looked at."""
+    page, pages, width = 16, 40, 20
+    keep = torch.empty((1, 2 ** 31 - 1), dtype=torch.int32, device=DEV)
+    room, rng = width * page, np.random.default_rng(3)
+    table = rng.permutation(pages)[:width].reshape(1, width).astype(np.int32)
+    first = np.sort(rng.permutation(room)[:200])
+    first = np.concatenate([first, np.arange(room - 200) + room]).astype(np.int32)
+    keep[0, :room] = ints(first)
+    for start in (0, 7):
+        k, v = (filled(pages, 2, page, 64, BF, x, i) for i, x in enumerate(("head", "token")))
+        moves = compact(table, [start], first[None], [room], page, pages)
+        assert len(moves) > 100
+        want = [moved(x, moves) for x in (k, v)]
+        bd.basa_cache_compact(bd.PagedCache(k, v), ints(table), ints([start]), keep, ints([2 ** 31 - 1]))
+        for x, w in zip((k, v), want):
+            assert torch.equal(bits(by_slot(x)), bits(w))
+
+
 # ---------------------------------------------------------------- forks and copies
 def _fork_check(lens, parents, n_free, page, seed, width=None):
     rng = np.random.default_rng(seed)
