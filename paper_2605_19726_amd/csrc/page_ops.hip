@@ -331,7 +331,8 @@ __device__ __forceinline__ void mark_rows(const FreeArgs& a, const int32_t* row,
   int most = held[0];
 #pragma unroll
   for (int r = 1; r < kRows; ++r) most = max(most, held[r]);
-  for (int p0 = threadIdx.x & 63; p0 < most + 63; p0 += 64 * kEntries) {         // (as many turns for every lane)
+  for (int first = 0; first < most; first += 64 * kEntries) {                    // (as many turns for every lane)
+    const int p0 = first + (threadIdx.x & 63);
     int id[kRows][kEntries];
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
