@@ -362,7 +362,8 @@ basa_status basa_decode_attn(const basa_tensor* q, const basa_tensor* k_pages, c
  * A step (basa_page_tables) in which sequence i gets n_i tokens, rows cu_seqlens[i] .. cu_seqlens[i + 1] - 1 of the packed batch.  They may be a tree: token r follows
  * token parents[r] of its sequence's new ones, or the context.  They enter the pages in their order (basa_cache_append), attend to the context and their
  * own ancestors (basa_tree_attn), and once some are accepted, the kept ones are moved together (basa_cache_compact) and the sequence is
- * as long as that.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending.  n_seq is up to 2^22.
+ * as long as that.  cu_seqlens: DEVICE, int32 [n_seq + 1], ascending; of offsets that do not ascend it is not defined which rows of the outputs are written, or with
+ * what.  n_seq is up to 2^22.
  */
 
 /*

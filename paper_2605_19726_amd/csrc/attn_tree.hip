@@ -70,13 +70,11 @@ constexpr int kWindow = 256;                // tokens whose places in the cache 
 // those of all parts of a row, 1024 at most, are a number.)
 constexpr float kRise = 8.f, kLarge = 0x1p117f;
 
+// n < 0: the offsets do not ascend.  Then nothing is done, since rows that several sequences have could be more than the axis has places for.
 struct Sequence { int len, row0, n; };
 __device__ __forceinline__ Sequence sequence_of(const TreeArgs& a, int b) {
-  Sequence s;
-  s.len = min(max(a.lens[b], 0), a.row_tokens);
-  s.row0 = min(max(a.cu[b], 0), a.tokens);
-  s.n = max(min(a.cu[b + 1], a.tokens) - s.row0, 0);
-  return s;
+  const PackedRows rows = packed_rows(a.cu[b], a.cu[b + 1], a.tokens);
+  return {min(max(a.lens[b], 0), a.row_tokens), rows.row0, rows.n};
 }
 constexpr int kMostRuns = 1024, kMostRows = 256;
 __device__ __forceinline__ int pack_cut(int first, int last, int row) { return first + kMostRuns * (last + kMostRuns * row); }
@@ -522,18 +520,23 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
   if (a.n <= kPlanBatch) {                        // a few sequences to a lane
     const int each = (a.n + 63) / 64;
     int mine = 0;
+    bool falls = false;
     if (each == 1) {
       if (lane < a.n) {
         mine_of = sequence_of(a, lane);
         mine = all_places(mine_of);
+        falls = mine_of.n < 0;
       }
     } else {                                      // (their lengths asked for at once)
 #pragma unroll
       for (int i = 0; i < kPlanBatch / 64; ++i) {
-        const int at = lane * each + i, places = all_places(sequence_of(a, min(at, a.n - 1)));
-        mine += i < each && at < a.n ? places : 0;
+        const int at = lane * each + i;
+        const Sequence s = sequence_of(a, min(at, a.n - 1));
+        mine += i < each && at < a.n ? all_places(s) : 0;
+        falls |= s.n < 0;
       }
     }
+    if (__ballot(falls)) return;
     const int upto = (int)wave_scan((uint32_t)mine, sum_of);
     of_head = __builtin_amdgcn_readlane(upto, 63);
     if (kSplit) run = (of_head * a.heads_kv + a.runs - 1) / a.runs;
@@ -560,7 +563,7 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
 
   for (int pos = begin; pos < end;) {
     if (b >= a.n) {
-      if (++kvh >= a.heads_kv) return;            // (offsets that do not ascend may have places for no one)
+      if (++kvh >= a.heads_kv) return;
       b = 0;
     }
     Sequence seq;
@@ -809,25 +812,32 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
 
 // First places of many sequences: one workgroup, a run of sequences to a thread.  (Up to kPlanBatch a launch less: 64 sequences 12.1 us in all.)
 __global__ __launch_bounds__(1024) void tree_plan_kernel(TreeArgs a, int step, int tile, bool split) {
-  __shared__ int wave_sum[16];
+  __shared__ int wave_sum[16], wave_falls[16];
   const int tid = threadIdx.x, each = (a.n + 1023) / 1024, i0 = min(tid * each, a.n), i1 = min(i0 + each, a.n);
+  bool falls = false;
   auto places = [&](int i) {
     const Sequence s = sequence_of(a, i);
+    falls |= s.n < 0;
     return tree_units(s.n * a.group, tile) * (split ? tree_steps(s.len, step) + tree_lead(step) : 1);
   };
   int mine = 0;
   for (int i = i0; i < i1; ++i) mine += places(i);
   const int upto = (int)wave_scan((uint32_t)mine, sum_of);
-  if ((tid & 63) == 63) wave_sum[tid >> 6] = upto;
+  const bool any_falls = __ballot(falls) != 0;
+  if ((tid & 63) == 63) {
+    wave_sum[tid >> 6] = upto;
+    wave_falls[tid >> 6] = any_falls;
+  }
   asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   __syncthreads();
-  int at = upto - mine;
+  int at = upto - mine, fall = 0;
   for (int w = 0; w < tid >> 6; ++w) at += wave_sum[w];
+  for (int w = 0; w < 16; ++w) fall |= wave_falls[w];
   for (int i = i0; i < i1; ++i) {
     a.first_place[i] = at;
     at += places(i);
   }
-  if (tid == 1023) a.first_place[a.n] = at;
+  if (tid == 1023) a.first_place[a.n] = fall ? 0 : at;
 }
 
 // The pieces of a row that more than one workgroup had a part in, added up, a wave to a row: 4 numbers to a lane, a part to every d / 4 lanes, four of them asked for at once.  In the

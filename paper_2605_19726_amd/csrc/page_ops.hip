@@ -24,7 +24,8 @@ __global__ __launch_bounds__(256) void tree_masks_kernel(const int32_t* parents,
   extern __shared__ __attribute__((aligned(16))) uint64_t run_bits[];      // [64 words], then the ways out
   int* const way_out = reinterpret_cast<int*>(run_bits + 64 * words);
   const int tid = threadIdx.x, lane = tid & 63;
-  const int row0 = min(max(cu[blockIdx.x], 0), tokens), n = max(min(cu[blockIdx.x + 1], tokens) - row0, 0), fit = min(n, 64 * words);
+  const PackedRows rows = packed_rows(cu[blockIdx.x], cu[blockIdx.x + 1], tokens);
+  const int row0 = rows.row0, n = max(rows.n, 0), fit = min(n, 64 * words);
   for (int run = tid >> 6; run * 64 < fit; run += 4) {
     const int r = run * 64 + lane;
     int p = r < fit ? parents[row0 + r] : -1;

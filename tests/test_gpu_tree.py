@@ -433,6 +433,69 @@ def test_offsets_that_do_not_ascend_stay_in_bounds():
             torch.cuda.synchronize()
 
 
+class Guarded:
+    """A tensor in the middle of a larger one, and whether what lies around it is as it was."""
+
+    def __init__(self, shape, dtype, fill=0x5b, guard=2 ** 20):
+        size = math.prod(shape) * torch.empty(0, dtype=dtype).element_size()
+        self.all = torch.full((guard + size + guard,), fill, dtype=torch.uint8, device=DEV)
+        self.guard, self.size, self.fill = guard, size, fill
+        self.t = self.all[guard:guard + size].view(dtype).view(shape)
+
+    def untouched(self):
+        return bool((self.all[:self.guard] == self.fill).all()) and bool((self.all[self.guard + self.size:] == self.fill).all())
+
+
+def _run_guarded(c, table, cu):
+    """The C call on outputs and a workspace, of the size that it asks for, with guards around them, and on the inputs, which it leaves as they are."""
+    cache, n = c.cache(), len(cu) - 1
+    table, lens, cu = ints(table), ints(c.lens), ints(cu)
+    need = bd.tree_workspace_size(c.q, cache, table)
+    out, lse, ws = Guarded(c.q.shape, c.q.dtype), Guarded((c.T, c.q.shape[1]), F32), Guarded((need,), torch.uint8)
+    inputs = (c.q, c.k, c.v, table, lens, cu) + (() if c.masks is None else (c.masks,))
+    before = [x.clone() for x in inputs]
+    words, stride = (0, 0) if c.masks is None else (c.masks.shape[1], c.masks.stride(0))
+    hq, d = c.q.shape[1:]
+    bd._launch(bd.load().basa_tree_attn, cache.device, bd._new_rows_desc(c.q, "q", cache), cache._kd, cache._vd, table.data_ptr(), table.shape[1], table.stride(0),
+               lens.data_ptr(), cu.data_ptr(), n, None if c.masks is None else c.masks.data_ptr(), words, stride, out.t.data_ptr(), None, lse.t.data_ptr(), ws.t.data_ptr(), need)
+    torch.cuda.synchronize()
+    assert out.untouched() and lse.untouched() and ws.untouched()
+    for x, b in zip(inputs, before):
+        assert torch.equal(bits(x) if x.is_floating_point() else x, bits(b) if b.is_floating_point() else b)
+    return out.t, lse.t
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (F32, 64)])
+@pytest.mark.parametrize("n,new,width", [(3, 8, 4), (3, 8, 60), (3, 70, 300), (600, 3, 8), (600, 3, 40)])
+def test_nothing_is_written_outside_the_outputs_and_the_workspace(dtype, d, n, new, width):
+    """One launch and cut, offsets summed up by a wave and by a kernel; offsets that ascend, and ones that do not."""
+    rng = np.random.default_rng(n + width)
+    lens = rng.integers(new, min(16 * width, 1500) + 1, n).tolist()
+    c = Case(dtype, d, 4, 2, 16, lens, [new] * n, 5, width=width, around=(0, 0))
+    c.check(*_run_guarded(c, c.table, c.cu))
+    T = c.T
+    wild = [rng.integers(-2 ** 31, 2 ** 31 - 1, n + 1), rng.permutation(T + 50)[:n + 1] - 20 if T + 50 > n else rng.integers(-20, T + 30, n + 1), np.full(n + 1, T), np.full(n + 1, -5),
+            np.arange(n + 1)[::-1] * new, np.where(np.arange(n + 1) % 2 == 0, 0, T), np.where(np.arange(n + 1) % 2 == 0, -2 ** 31, 2 ** 31 - 1)]
+    masks = c.masks
+    for cu in wild:
+        for m in (masks, None):
+            c.masks = m
+            _run_guarded(c, c.table, cu)
+
+
+def test_masks_are_written_in_their_rows_alone():
+    for T, n, words in ((40, 2, 1), (300, 4, 3)):
+        rng = np.random.default_rng(T)
+        parents = ints(np.arange(T) - 1)
+        for cu in ([0] + [T] * n, [T // 2] * (n + 1), np.sort(rng.integers(0, T, n + 1)), rng.integers(-2 ** 31, 2 ** 31 - 1, n + 1), np.arange(n + 1)[::-1] * (T // n), [-5] * n + [2 ** 31 - 1],
+                   rng.integers(-T, 2 * T, n + 1), np.where(np.arange(n + 1) % 2 == 0, T // 2, -2 ** 31)):
+            masks, depths = Guarded((T, words + 1), torch.int64), Guarded((T,), torch.int32)
+            between = masks.t[:, words].clone()
+            bd.basa_tree_masks(parents, ints(cu), words, out=(masks.t[:, :words], depths.t))
+            torch.cuda.synchronize()
+            assert masks.untouched() and depths.untouched() and torch.equal(masks.t[:, words], between)
+
+
 def _spread(x, stride_b, stride_h, stride_l):
     """The same pages far apart, in storage of which nothing else is ever written."""
     n, h, t, d = x.shape

@@ -23,6 +23,10 @@ int main() {
     if (!std::strcmp(what, "tree") && std::scanf("%llu %llu %lld", &x, &y, &a) == 3) std::printf("%u\n", basa::tree_bits(x, y, a));
     if (!std::strcmp(what, "steps") && std::scanf("%lld %lld", &a, &b) == 2) std::printf("%d\n", basa::tree_steps(a, b));
     if (!std::strcmp(what, "units") && std::scanf("%lld %lld", &a, &b) == 2) std::printf("%d\n", basa::tree_units(a, b));
+    if (!std::strcmp(what, "rows") && std::scanf("%lld %lld %lld", &a, &b, &c) == 3) {
+      const basa::PackedRows r = basa::packed_rows(a, b, c);
+      std::printf("%d %d\n", r.row0, r.n);
+    }
     if (!std::strcmp(what, "lead") && std::scanf("%lld", &a) == 1) std::printf("%d\n", basa::tree_lead(a));
     if (!std::strcmp(what, "ends") && std::scanf("%lld %lld %lld %lld", &a, &b, &c, &d) == 4)
       std::printf("%d %d\n", basa::decode_first_group(a, c, d), basa::decode_last_group(a, b, c, d));
@@ -63,6 +67,16 @@ def test_words_of_a_mask_as_the_bits_of_a_step(plan):
             # tokens before the new ones are seen by all
             want.append(sum(1 << i for i in range(32) if at + i < 0 or words[(at + i) // 64] >> ((at + i) % 64) & 1))
     assert plan(asked) == want
+
+
+def test_rows_of_a_sequence_are_rows_of_the_batch(plan):
+    """Whatever the offsets are, also where their difference is no 32-bit number: within [0, tokens], less than none where they do not ascend."""
+    ends = [-2 ** 31, -2 ** 31 + 1, -1800, -1, 0, 1, 5, 1799, 1800, 1801, 2 ** 30, 2 ** 31 - 1]
+    asked = [("rows", a, b, t) for a in ends for b in ends for t in (1, 6, 1800, 2 ** 30)]
+    got = plan(asked)
+    for (_, a, b, t), row0, n in zip(asked, got[::2], got[1::2]):
+        first, end = (max(0, min(x, t)) for x in (a, b))
+        assert (row0, n) == (first, end - first) and (n >= 0 or b < a)
 
 
 @pytest.mark.parametrize("step", [16, 32])
