@@ -168,6 +168,22 @@ def test_a_sequence_that_was_not_served_keeps_nothing_and_writes_into_no_page_of
     assert torch.minimum(lens + kept, step.lens).tolist() == [20, need]
 
 
+def test_lists_that_are_none_leave_other_sequences_alone_in_k_and_v():
+    """Descending, repeated, far and negative entries, of short lists and of long ones: the pages of no sequence, and of one without entries, hold what they held."""
+    rng = np.random.default_rng(7)
+    for most in (8, 300):
+        k, v = (filled(60, 2, 16, 64, BF, x, i) for i, x in enumerate(("head", "token")))
+        before = [by_slot(x) for x in (k, v)]
+        table = ints(np.arange(60).reshape(3, 20))[:2]
+        keep = rng.choice([-2 ** 31, -7, 0, 3, 9, 40, 319, 320, 2 ** 31 - 1], (2, most))
+        keep[:, most // 2:] = rng.integers(0, 400, (2, most - most // 2))
+        for start in ([0, 0], [2 ** 31 - 1, 5], [300, -2 ** 31]):
+            for lens in (None, ints([320, 320]), ints([2 ** 31 - 1, -2 ** 31])):
+                bd.basa_cache_compact(bd.PagedCache(k, v), table, ints(start), ints(keep), ints([most, 0]), lens)
+        for x, b in zip((k, v), before):
+            assert torch.equal(bits(by_slot(x)[320:]), bits(b[320:]))
+
+
 def test_lists_that_are_longer_than_a_row():
     """As many entries as a call can name, all of them counted: those that a row has room for matter, and no others are looked at."""
     page, pages, width = 16, 40, 20

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paged_util import new_tables, rows_of, store
+from paged_util import HALF_STEP, decode_tolerance, new_tables, rows_of, store
 from test_gpu_paged import BF, DEV, F32, bits, ints, randn
 from tree_util import ancestors, check_tree, mask_words, random_parents
 from paper_2605_19726_amd import binding as bd
@@ -494,6 +494,34 @@ def test_masks_are_written_in_their_rows_alone():
             bd.basa_tree_masks(parents, ints(cu), words, out=(masks.t[:, :words], depths.t))
             torch.cuda.synchronize()
             assert masks.untouched() and depths.untouched() and torch.equal(masks.t[:, words], between)
+
+
+# more sequences than a workgroup of the sum over them has threads, and than two rounds of the search tell apart; runs of empty ones, the last one without rows
+@pytest.mark.parametrize("dtype,d,n,new,width", [(BF, 64, 1500, 3, 8), (F32, 64, 1500, 3, 40), (BF, 128, 5000, 2, 4), (BF, 128, 5000, 2, 40), (F32, 128, 5000, 2, 40), (BF, 128, 600, 80, 30),
+                                                 (F32, 64, 600, 20, 30), (BF, 64, 600, 50, 8)])
+def test_very_many_sequences(dtype, d, n, new, width):
+    rng = np.random.default_rng(n + width)
+    count = rng.integers(0, new + 1, n)
+    for a in (0, n // 3, n - 70):
+        count[a:a + 70] = 0
+    count[-2] = new
+    lens = np.maximum(rng.integers(0, 16 * min(width, 10) + 1, n), count)
+    lens[rng.random(n) < 0.02] = 16 * width
+    c = Case(dtype, d, 8, 2, 16, lens.tolist(), count.tolist(), 11, width=width)
+    out, lse = c.run()
+    table, cu = ints(c.table), c.cu
+    # every row against calls of up to 256 sequences: either is off from 64 bits by what a call may be, and rounded once
+    norm = lambda x: float(x.float().nan_to_num(0).norm(dim=-1).max())  # noqa: E731
+    tol, tol_lse = decode_tolerance(dtype, int(lens.max()), d, norm(c.q) * norm(c.k) / math.sqrt(d), float(c.v.float().nan_to_num(0).abs().max()))
+    for a in range(0, n, 256):
+        b = min(a + 256, n)
+        rows = slice(int(cu[a]), int(cu[b]))
+        part, part_lse = bd.basa_tree_attn(c.q[rows], c.cache(), table[a:b], ints(lens[a:b]), ints(cu[a:b + 1] - cu[a]), c.masks[rows], want_lse=True)
+        x, y, e, f = out[rows].double(), part.double(), lse[rows].double(), part_lse.double()
+        assert bool(((x - y).abs() <= 2 * tol + HALF_STEP[dtype] * 1.01 * (x.abs() + y.abs())).all())
+        assert torch.equal(torch.isinf(e), torch.isinf(f)) and bool(((e - f).abs()[torch.isfinite(e)] <= 2 * tol_lse).all())
+    for i in sorted({70, n // 3 - 1, n // 3 + 70, n - 71, n - 2, *rng.integers(0, n, 40).tolist()}):
+        check_tree(out, lse, c.q, c.k, c.v, c.table, c.lens, c.cu, c.seen, f"{dtype} {d} {n}", only=(i, list(range(c.new[i]))))
 
 
 def _spread(x, stride_b, stride_h, stride_l):
