@@ -520,12 +520,12 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
   if (a.n <= kPlanBatch) {                        // a few sequences to a lane
     const int each = (a.n + 63) / 64;
     int mine = 0;
-    bool falls = false;
+    int fewest = 0;
     if (each == 1) {
       if (lane < a.n) {
         mine_of = sequence_of(a, lane);
         mine = all_places(mine_of);
-        falls = mine_of.n < 0;
+        fewest = mine_of.n;
       }
     } else {                                      // (their lengths asked for at once)
 #pragma unroll
@@ -533,10 +533,10 @@ __global__ __launch_bounds__(64 * kWaves, (Geometry<kBf16, kD, kWaves, kSplit>::
         const int at = lane * each + i;
         const Sequence s = sequence_of(a, min(at, a.n - 1));
         mine += i < each && at < a.n ? all_places(s) : 0;
-        falls |= s.n < 0;
+        fewest = min(fewest, s.n);
       }
     }
-    if (__ballot(falls)) return;
+    if (__ballot(fewest < 0)) return;
     const int upto = (int)wave_scan((uint32_t)mine, sum_of);
     of_head = __builtin_amdgcn_readlane(upto, 63);
     if (kSplit) run = (of_head * a.heads_kv + a.runs - 1) / a.runs;

@@ -75,8 +75,8 @@ BASA_HD int tree_units(int rows, int tile) { return (rows + tile - 1) / tile; }
 // Rows [from, to) of a packed batch of `tokens` rows, of what it has of them: the first, and how many.  Less than none: offsets that do not ascend.
 struct PackedRows { int row0, n; };
 BASA_HD PackedRows packed_rows(int from, int to, int tokens) {
-  const int row0 = from < 0 ? 0 : from < tokens ? from : tokens, end = to < 0 ? 0 : to < tokens ? to : tokens;
-  return {row0, end - row0};
+  const int first = from > 0 ? from : 0, last = to > 0 ? to : 0, row0 = first < tokens ? first : tokens;
+  return {row0, (last < tokens ? last : tokens) - row0};
 }
 // What 32 drafted tokens from `at` on (negative: tokens of the context, which all see) the token `t` of a chain sees: those up to itself.
 BASA_HD uint32_t chain_bits(int t, int at) {
