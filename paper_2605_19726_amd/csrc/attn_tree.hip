@@ -12,9 +12,10 @@
 //   - S^T = K Q^T and O^T = V^T P^T: a lane has the same row in the scores, the weights and the output, so that weights are operands where they are, and the maximum and
 //     the sum of a row are two lanes' (four).
 //   - Weights enter the second product as two bf16 numbers, the upper half of the f32 and the rest: three products of matrix units for two of the formula, and the only rounding to
-//     8 bits is the output's.  (131072 tokens, 64 new ones, 256 rows: 229 us, 911 TF executed of the 1276 that a large product of matrices runs at.  Half of the cycles
-//     the matrix units work, and half the vector units; to have them overlap more, by the next step's scores during this one's products, by waves of different
-//     priority, by one barrier to two or four steps, leaves the time as it is (225 to 240): the clock falls to 1.8 GHz.)
+//     8 bits is the output's.  (131072 tokens, 64 new ones, 256 rows: 229 us, 900 TF executed of the 1276 that a large product of matrices runs at.  48% of the cycles
+//     the matrix units work, and in 42% there are other vector instructions: they follow each other.  The next step's scores during this one's products, waves of
+//     different priority, one barrier to two or four steps leave the time as it is (225 to 240).  There are 1.13 LDS instructions to a product; a wave of 64 rows, which
+//     would halve them, has not been tried.)
 //   - Work is cut on one axis (paged_plan.hpp): KV head by KV head, in each the sequences, in each the tiles of rows, each with a place for every step and some for what a
 //     piece costs by itself; every workgroup finds its run of places from the lengths.  Pieces are added up by a second kernel where their L2 has them.
 #include <algorithm>
@@ -470,8 +471,9 @@ struct Rows<false, kD> {
 };
 
 // A workgroup has a wave for every kRows rows of a tile; each takes every token (every second step, where two waves share rows).  Of a ring of kStages steps in the LDS one is worked on, the others are on
-// their way there: 64 KB for a workgroup of two or four waves, two to a compute unit, 128 KB for one of eight.  Short sequences of few rows want more workgroups, not more
-// steps ahead: two steps in the ring and four workgroups (64 sequences of 60 tokens, bf16, d = 128: 16.4 -> 12.1 us; 512 of them 110 -> 87).
+// their way there.  A step has 16 KB at d = 128, 8 KB at 64, in either type.  Eight waves have eight steps, one workgroup to a compute unit; four waves 64 KB, two workgroups.  Two waves
+// have four steps: 64 KB and two workgroups of cut sequences at d = 128, 32 KB and four workgroups at 64.  Short sequences at d = 128, which are not cut, want
+// more workgroups, not more steps ahead: two steps and four workgroups (64 sequences of 60 tokens, bf16: 16.4 -> 12.1 us; 512 of them 110 -> 87, and 77 in a later run).
 template <bool kBf16, int kD, int kWaves, bool kSplit>
 struct Geometry {
   using R = Rows<kBf16, kD>;
